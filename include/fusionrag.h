@@ -322,6 +322,66 @@ fr_status fr_decode_attn(fr_ctx* ctx, const void* q, int32_t n_queries, const vo
 fr_status fr_mark_stale_rows(fr_ctx* ctx, uint32_t* stale_bits, int64_t n_words, const int32_t* rows, int32_t n_rows,
                              int32_t clear, void* stream);
 
+/* ---- A serving step over a paged cache.  A server that appends to many requests at once keeps their K/V in pages of
+ * page_rows rows, taken from a free list as the requests grow (the exclusive pages of Sec. 4.3, allotted piece by piece).
+ *   k_pages, v_pages  dev [n_pages][page_rows][Hkv][d]; row r of page p is row p * page_rows + r of the cache (its "slot")
+ *   block_table       dev [n_requests][max_blocks] int32: entry j of request b is the page of its positions
+ *                     j * page_rows .. (j + 1) * page_rows - 1
+ *   cached_len        dev [n_requests] int32: positions of each request that the pages hold before the step
+ *   q_offsets         dev [n_requests + 1] int32: row t of the step belongs to request b for q_offsets[b] <= t < q_offsets[b + 1]
+ *                     and is that request's position cached_len[b] + t - q_offsets[b].  Ascending
+ * A step is fr_page_tables, then per layer fr_paged_append and fr_paged_attn; the lengths stay on the device, so a captured
+ * step is replayed for other lengths.  The context's max_tokens bounds none of this; max_blocks * page_rows and n_tokens
+ * are at most 2^30, n_pages * page_rows at most 2^31 - 1 (FR_ERR_UNSUPPORTED beyond). */
+#define FR_PAGED_MAX_REQUESTS 4096
+
+/* Tables of a step from the requests' lengths.  Request b brings new_len[b] rows: they are rows q_offsets[b] ..
+ * of the step (rows beyond n_tokens are left out: q_offsets ends there), at positions cached_len[b] .. .  The pages that those
+ * positions need beyond the ceil(cached_len[b] / page_rows) that the request holds are taken from the free list in the order of
+ * the requests and their positions, and entered in its row of block_table; no other entry changes.
+ *   cached_len, new_len  dev [n_requests] int32 (a negative one counts as 0)
+ *   free_pages   dev [n_free] int32 page numbers; free_start dev [1] int32: index of the first one to be taken, or NULL: 0
+ *   block_table  dev [n_requests][max_blocks] int32, read and written
+ *   q_offsets    dev [n_requests + 1] int32
+ *   positions    dev [n_tokens] int32: of each row; 0 for rows behind the last request's
+ *   slots        dev [n_tokens] int32: the cache row of each row; -1 for rows behind the last request's, for positions beyond
+ *                max_blocks pages, and for those whose page the free list no longer had (its table entry is -1 then)
+ *   pages_needed dev [1] int32: pages that the call takes, those that the list lacked included, or NULL.  The caller moves
+ *                free_start on by it before the next step
+ * Everything is a function of the inputs: a call that is repeated gives the same tables. */
+fr_status fr_page_tables(fr_ctx* ctx, const int32_t* cached_len, const int32_t* new_len, int32_t n_requests, int32_t page_rows,
+                         const int32_t* free_pages, int32_t n_free, const int32_t* free_start, int32_t* block_table,
+                         int32_t max_blocks, int32_t n_tokens, int32_t* q_offsets, int32_t* positions, int32_t* slots,
+                         int32_t* pages_needed, void* stream);
+
+/* A step's rows into the pages: k_pages[slots[t]] = R(positions[t]) k_new[t], v_pages[slots[t]] = v_new[t], and
+ * q_out[t] = R(positions[t]) q[t], with R the rotary embedding of the context's layer description.
+ *   q            dev [n_tokens, Hq, d], not rotated, or NULL: keys and values only (q_out is NULL too)
+ *   q_out        dev [n_tokens, Hq, d]; may equal q
+ *   k_new, v_new dev [n_tokens, Hkv, d], not within the pages
+ *   positions    dev [n_tokens] int32, or NULL: nothing is rotated, keys are stored bit for bit (rows of fr_qkv_rope)
+ *   slots        dev [n_tokens] int32; a row whose slot lies outside the cache (such as -1) is stored nowhere, its q_out is written.
+ *                No slot of the cache occurs twice
+ * Arithmetic: fp32 on cos/sin rounded from fp64; output rounded to dtype (nearest-even). */
+fr_status fr_paged_append(fr_ctx* ctx, const void* q, const void* k_new, const void* v_new, const int32_t* positions,
+                          const int32_t* slots, int32_t n_tokens, void* k_pages, void* v_pages, int32_t n_pages,
+                          int32_t page_rows, void* q_out, void* stream);
+
+/* Attention of a step's rows over the pages: the row at position p of request b attends to the request's positions 0 .. p
+ * (its own and those of its chunk included: append first).  One call serves decoding (a row per request), drafted tokens, chunks of
+ * prompts and whole prompts side by side.
+ *   q            dev [n_tokens, Hq, d], rotated
+ *   max_new      no request of the call has more rows than this (rows of a request beyond it are not computed)
+ *   out          dev [n_tokens, Hq, d];  lse_out dev [n_tokens, Hq] fp32 natural-log normalisers, or NULL
+ * Rows of no request (q_offsets[n_requests] .. n_tokens - 1) are left as they were.  A position whose table entry is not a page
+ * of the cache (0 .. n_pages - 1), or that lies beyond max_blocks pages, is invisible; a row that sees nothing at all (also: at a
+ * negative position) has out = 0 and lse = -inf.  What a row does not see has no influence on it, whatever it holds.
+ * Arithmetic: products of dtype inputs accumulated in fp32, softmax in fp32, out rounded to dtype. */
+fr_status fr_paged_attn(fr_ctx* ctx, const void* q, const int32_t* q_offsets, const int32_t* cached_len, int32_t n_requests,
+                        int32_t n_tokens, int32_t max_new, const void* k_pages, const void* v_pages, int32_t n_pages,
+                        int32_t page_rows, const int32_t* block_table, int32_t max_blocks, void* out, float* lse_out,
+                        void* stream);
+
 /* Write-back (Sec. 4.3): k_cache[q_index[r]] = k_new[r], v_cache[q_index[r]] = v_new[r],
  * bit-exact copies; other rows are not touched.  Shapes as above. */
 fr_status fr_kv_scatter(fr_ctx* ctx, const void* k_new, const void* v_new, const int32_t* q_index,

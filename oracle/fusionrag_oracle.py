@@ -382,3 +382,77 @@ def selective_prefill_layer(h: np.ndarray, q_index: np.ndarray, k_cache: np.ndar
     act = r(linear_swiglu(x2, weights["w_gate_up"]))
     h2 = r(linear(act, weights["w_down"], h1))
     return h2, k_new, v_new
+
+
+# --------------------------------------------------------------------------------------
+# A serving step over a paged cache: the exclusive pages of Sec. 4.3 allotted in pages of a few rows
+# --------------------------------------------------------------------------------------
+def page_tables(cached_len, new_len, page_rows: int, free_pages, free_start: int, block_table: np.ndarray, n_tokens: int):
+    """Tables of a step, request by request: (block_table, q_offsets, positions, slots, pages_needed)."""
+    table = np.array(block_table, dtype=np.int64)
+    width = table.shape[1]
+    positions, slots = np.zeros(n_tokens, dtype=np.int64), np.full(n_tokens, -1, dtype=np.int64)
+    offsets, taken, t = [0], 0, 0
+    for b, (c, n) in enumerate(zip(cached_len, new_len)):
+        c, n = max(int(c), 0), min(max(int(n), 0), n_tokens - t)
+        held = -(-c // page_rows)
+        for i in range(n):
+            p = c + i
+            j = p // page_rows
+            if j < width:
+                if j >= held and (i == 0 or p % page_rows == 0):      # the first position of a page not held
+                    at = free_start + taken
+                    table[b, j] = free_pages[at] if 0 <= at < len(free_pages) else -1
+                    taken += 1
+                if table[b, j] >= 0:
+                    slots[t + i] = table[b, j] * page_rows + p % page_rows
+            positions[t + i] = p
+        t += n
+        offsets.append(t)
+    return table, np.array(offsets), positions, slots, taken
+
+
+def paged_append(q, k_new, v_new, positions, slots, k_pages: np.ndarray, v_pages: np.ndarray, base: float,
+                 layout: str = "interleaved", index_base: int = 0):
+    """(q_out, k_pages, v_pages) after a step's rows went into the pages [n_pages, page_rows, Hkv, d]; positions = None: not rotated."""
+    if positions is not None:
+        k_new = rope_rotate(k_new, positions, base, layout, index_base)
+        q = rope_rotate(q, positions, base, layout, index_base) if q is not None else None
+    kp, vp = np.array(k_pages, dtype=F64), np.array(v_pages, dtype=F64)
+    rows = kp.shape[0] * kp.shape[1]
+    kf, vf = kp.reshape(rows, *kp.shape[2:]), vp.reshape(rows, *vp.shape[2:])
+    for t, s in enumerate(slots):
+        if 0 <= s < rows:
+            kf[s], vf[s] = k_new[t], v_new[t]
+    return q, kp, vp
+
+
+def paged_attn(q, q_offsets, cached_len, k_pages, v_pages, block_table, rows=None):
+    """Attention of a step's rows over their requests' pages (Sec. 2.1, softmax of the scaled logits): {row: (out [Hq, d], lse [Hq],
+    mass [Hq, d], spread [Hq])} of the listed rows (default: all), mass = sum of weight x |value| and spread = the largest sum of
+    |q_c k_c| / sqrt(d) over the keys, which bound what roundings can do."""
+    n_pages, P, Hkv, d = k_pages.shape
+    Hq = q.shape[1]
+    G = Hq // Hkv
+    got = {}
+    for b in range(len(cached_len)):
+        for t in range(int(q_offsets[b]), int(q_offsets[b + 1])):
+            if rows is not None and t not in rows:
+                continue
+            p = int(cached_len[b]) + t - int(q_offsets[b])
+            j = np.arange(min(p + 1, block_table.shape[1] * P) if p >= 0 else 0)
+            page = np.asarray(block_table)[b, j // P] if len(j) else j
+            there = (page >= 0) & (page < n_pages)
+            page, at = page[there], (j % P)[there]
+            out, lse = np.zeros((Hq, d)), np.full(Hq, -np.inf)
+            mass, spread = np.zeros((Hq, d)), np.zeros(Hq)
+            if len(page):
+                K, V = np.asarray(k_pages[page, at], dtype=F64), np.asarray(v_pages[page, at], dtype=F64)
+                for h in range(Hq):
+                    x = np.asarray(q[t, h], dtype=F64)
+                    s = K[:, h // G] @ x / math.sqrt(d)
+                    w = np.exp(s - s.max())
+                    out[h], lse[h] = (w / w.sum()) @ V[:, h // G], s.max() + math.log(w.sum())
+                    mass[h], spread[h] = (w / w.sum()) @ np.abs(V[:, h // G]), (np.abs(K[:, h // G]) @ np.abs(x)).max() / math.sqrt(d)
+            got[t] = (out, lse, mass, spread)
+    return got

@@ -18,6 +18,7 @@ FR_ROPE_INTERLEAVED, FR_ROPE_HALF = 0, 1
 FR_NORM_PER_CHUNK, FR_NORM_GLOBAL, FR_NORM_RAW = 0, 1, 2
 FR_MAX_CHUNKS = 256
 FR_SELECT_STATIC_MAX_SCORES = 1 << 24
+FR_PAGED_MAX_REQUESTS = 4096
 STATUS_NAMES = {0: "FR_OK", 1: "FR_ERR_INVALID_ARG", 2: "FR_ERR_UNSUPPORTED", 3: "FR_ERR_WORKSPACE",
                 4: "FR_ERR_DEVICE"}
 FR_OPT_ATTN_SOFTMAX = 1
@@ -30,7 +31,7 @@ FR_DECODE_KERNEL_AUTO, FR_DECODE_KERNEL_GENERIC = 0, 1
 FR_ATTN_SOFTMAX_AUTO, FR_ATTN_SOFTMAX_RUNNING_MAX = 0, 1
 FR_ATTN_SPLIT_AUTO, FR_ATTN_SPLIT_OFF, FR_ATTN_SPLIT_ON = 0, 1, 2
 EXPORTS = ("fr_create", "fr_destroy", "fr_last_error", "fr_workspace_bytes", "fr_set_option", "fr_attn_kernel_times", "fr_topk_count", "fr_rope_shift",
-           "fr_score_select", "fr_score_select_shared", "fr_select_topk", "fr_select_topk_static", "fr_kv_deviation", "fr_sparse_prefill_attn", "fr_sparse_prefill_attn_writeback", "fr_sparse_prefill_attn_shared", "fr_shared_batch_workspace_bytes", "fr_sparse_prefill_attn_shared_batch", "fr_decode_attn", "fr_mark_stale_rows", "fr_kv_scatter", "fr_rmsnorm", "fr_linear",
+           "fr_score_select", "fr_score_select_shared", "fr_select_topk", "fr_select_topk_static", "fr_kv_deviation", "fr_sparse_prefill_attn", "fr_sparse_prefill_attn_writeback", "fr_sparse_prefill_attn_shared", "fr_shared_batch_workspace_bytes", "fr_sparse_prefill_attn_shared_batch", "fr_decode_attn", "fr_mark_stale_rows", "fr_page_tables", "fr_paged_append", "fr_paged_attn", "fr_kv_scatter", "fr_rmsnorm", "fr_linear",
            "fr_linear_swiglu", "fr_qkv_rope")
 
 
@@ -127,6 +128,12 @@ def _open(arr, shared_query) -> ctypes.CDLL:
     lib.fr_decode_attn.restype = i32
     lib.fr_mark_stale_rows.argtypes = [vp, vp, i64, vp, i32, i32, vp]
     lib.fr_mark_stale_rows.restype = i32
+    lib.fr_page_tables.argtypes = [vp, vp, vp, i32, i32, vp, i32, vp, vp, i32, i32, vp, vp, vp, vp, vp]
+    lib.fr_page_tables.restype = i32
+    lib.fr_paged_append.argtypes = [vp, vp, vp, vp, vp, vp, i32, vp, vp, i32, i32, vp, vp]
+    lib.fr_paged_append.restype = i32
+    lib.fr_paged_attn.argtypes = [vp, vp, vp, vp, i32, i32, i32, vp, vp, i32, i32, vp, i32, vp, vp, vp]
+    lib.fr_paged_attn.restype = i32
     lib.fr_kv_scatter.argtypes = [vp, vp, vp, vp, i32, vp, vp, i64, vp]
     lib.fr_kv_scatter.restype = i32
     lib.fr_rmsnorm.argtypes = [vp, vp, vp, i32, i32, ctypes.c_float, vp, vp]
@@ -324,6 +331,25 @@ class Context:
     def fr_mark_stale_rows(self, stale_bits, n_words: int, rows, n_rows: int, clear: bool = True, stream=None):
         self._check(self._lib.fr_mark_stale_rows(self._h, _ptr(stale_bits), int(n_words), _ptr(rows), int(n_rows),
                                                  int(bool(clear)), _stream(stream)))
+
+    def fr_page_tables(self, cached_len, new_len, n_requests: int, page_rows: int, free_pages, n_free: int, free_start, block_table,
+                       max_blocks: int, n_tokens: int, q_offsets, positions, slots, pages_needed=None, stream=None):
+        self._check(self._lib.fr_page_tables(self._h, _ptr(cached_len), _ptr(new_len), int(n_requests), int(page_rows),
+                                             _ptr(free_pages), int(n_free), _ptr(free_start), _ptr(block_table), int(max_blocks),
+                                             int(n_tokens), _ptr(q_offsets), _ptr(positions), _ptr(slots), _ptr(pages_needed),
+                                             _stream(stream)))
+
+    def fr_paged_append(self, q, k_new, v_new, positions, slots, n_tokens: int, k_pages, v_pages, n_pages: int, page_rows: int,
+                        q_out=None, stream=None):
+        self._check(self._lib.fr_paged_append(self._h, _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(positions), _ptr(slots),
+                                              int(n_tokens), _ptr(k_pages), _ptr(v_pages), int(n_pages), int(page_rows),
+                                              _ptr(q_out), _stream(stream)))
+
+    def fr_paged_attn(self, q, q_offsets, cached_len, n_requests: int, n_tokens: int, max_new: int, k_pages, v_pages, n_pages: int,
+                      page_rows: int, block_table, max_blocks: int, out, lse_out=None, stream=None):
+        self._check(self._lib.fr_paged_attn(self._h, _ptr(q), _ptr(q_offsets), _ptr(cached_len), int(n_requests), int(n_tokens),
+                                            int(max_new), _ptr(k_pages), _ptr(v_pages), int(n_pages), int(page_rows),
+                                            _ptr(block_table), int(max_blocks), _ptr(out), _ptr(lse_out), _stream(stream)))
 
     def fr_kv_scatter(self, k_new, v_new, q_index, R: int, k_cache, v_cache, L: int, stream=None):
         self._check(self._lib.fr_kv_scatter(self._h, _ptr(k_new), _ptr(v_new), _ptr(q_index), int(R), _ptr(k_cache),

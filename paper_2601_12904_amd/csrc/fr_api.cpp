@@ -820,6 +820,123 @@ fr_status fr_kv_scatter(fr_ctx* ctx, const void* k_new, const void* v_new, const
     return FR_OK;
 }
 
+// ---- a serving step over a paged cache ---------------------------------------------------------------
+
+namespace {
+bool bad4(const void* p) { return !p || (reinterpret_cast<uintptr_t>(p) & 3u); }
+bool bad16(const void* p) { return !p || !aligned16(p); }
+
+// Rows of a page and blocks of a table.
+fr_status check_table(fr_ctx* ctx, int32_t n_requests, int32_t page_rows, int32_t max_blocks) {
+    if (n_requests < 0) return fail(ctx, FR_ERR_INVALID_ARG, "n_requests = %d is negative", n_requests);
+    if (n_requests > FR_PAGED_MAX_REQUESTS)
+        return fail(ctx, FR_ERR_UNSUPPORTED, "n_requests = %d exceeds %d", n_requests, FR_PAGED_MAX_REQUESTS);
+    if (page_rows <= 0) return fail(ctx, FR_ERR_INVALID_ARG, "page_rows = %d is not positive", page_rows);
+    if (max_blocks < 0) return fail(ctx, FR_ERR_INVALID_ARG, "max_blocks = %d is negative", max_blocks);
+    if ((int64_t)max_blocks * page_rows > PAGED_MAX_POSITIONS)
+        return fail(ctx, FR_ERR_UNSUPPORTED, "max_blocks x page_rows = %lld exceeds 2^30 positions", (long long)max_blocks * page_rows);
+    return FR_OK;
+}
+fr_status check_tokens(fr_ctx* ctx, int32_t n_tokens) {
+    if (n_tokens < 0) return fail(ctx, FR_ERR_INVALID_ARG, "n_tokens = %d is negative", n_tokens);
+    if (n_tokens > PAGED_MAX_POSITIONS) return fail(ctx, FR_ERR_UNSUPPORTED, "n_tokens = %d exceeds 2^30", n_tokens);
+    return FR_OK;
+}
+fr_status check_pages(fr_ctx* ctx, int32_t n_pages, int32_t page_rows) {
+    if (n_pages < 0) return fail(ctx, FR_ERR_INVALID_ARG, "n_pages = %d is negative", n_pages);
+    if (page_rows <= 0) return fail(ctx, FR_ERR_INVALID_ARG, "page_rows = %d is not positive", page_rows);
+    if ((int64_t)n_pages * page_rows > INT32_MAX)
+        return fail(ctx, FR_ERR_UNSUPPORTED, "n_pages x page_rows = %lld exceeds 2^31 - 1 rows", (long long)n_pages * page_rows);
+    return FR_OK;
+}
+}  // namespace
+
+fr_status fr_page_tables(fr_ctx* ctx, const int32_t* cached_len, const int32_t* new_len, int32_t n_requests, int32_t page_rows,
+                         const int32_t* free_pages, int32_t n_free, const int32_t* free_start, int32_t* block_table,
+                         int32_t max_blocks, int32_t n_tokens, int32_t* q_offsets, int32_t* positions, int32_t* slots,
+                         int32_t* pages_needed, void* stream) {
+    if (!ctx) return FR_ERR_INVALID_ARG;
+    ctx->err.clear();
+    fr_status st = check_table(ctx, n_requests, page_rows, max_blocks);
+    if (st != FR_OK) return st;
+    if ((st = check_tokens(ctx, n_tokens)) != FR_OK) return st;
+    if (n_free < 0) return fail(ctx, FR_ERR_INVALID_ARG, "n_free = %d is negative", n_free);
+    if (n_requests > 0 && (bad4(cached_len) || bad4(new_len)))
+        return fail(ctx, FR_ERR_INVALID_ARG, "cached_len / new_len is NULL or not 4-byte aligned");
+    if ((n_requests > 0 && max_blocks > 0 && bad4(block_table)) || (n_free > 0 && bad4(free_pages)))
+        return fail(ctx, FR_ERR_INVALID_ARG, "block_table / free_pages is NULL or not 4-byte aligned");
+    if (bad4(q_offsets) || (n_tokens > 0 && (bad4(positions) || bad4(slots))))
+        return fail(ctx, FR_ERR_INVALID_ARG, "q_offsets / positions / slots is NULL or not 4-byte aligned");
+    if ((reinterpret_cast<uintptr_t>(free_start) & 3u) || (reinterpret_cast<uintptr_t>(pages_needed) & 3u))
+        return fail(ctx, FR_ERR_INVALID_ARG, "free_start / pages_needed must be 4-byte aligned");
+    if ((st = need_device(ctx)) != FR_OK) return st;
+    PageTablesArgs a;
+    a.cached_len = cached_len; a.new_len = new_len; a.n_requests = n_requests; a.page_rows = page_rows;
+    a.free_pages = free_pages; a.n_free = n_free; a.free_start = free_start;
+    a.block_table = block_table; a.max_blocks = max_blocks; a.n_tokens = n_tokens;
+    a.q_offsets = q_offsets; a.positions = positions; a.slots = slots; a.pages_needed = pages_needed;
+    hipError_t e = launch_page_tables(a, (hipStream_t)stream);
+    if (e != hipSuccess) return hip_fail(ctx, "page tables launch", e);
+    return FR_OK;
+}
+
+fr_status fr_paged_append(fr_ctx* ctx, const void* q, const void* k_new, const void* v_new, const int32_t* positions,
+                          const int32_t* slots, int32_t n_tokens, void* k_pages, void* v_pages, int32_t n_pages,
+                          int32_t page_rows, void* q_out, void* stream) {
+    if (!ctx) return FR_ERR_INVALID_ARG;
+    ctx->err.clear();
+    fr_status st = check_tokens(ctx, n_tokens);
+    if (st != FR_OK) return st;
+    if ((st = check_pages(ctx, n_pages, page_rows)) != FR_OK) return st;
+    if (n_tokens == 0) return FR_OK;
+    if (bad16(k_new) || bad16(v_new) || (n_pages > 0 && (bad16(k_pages) || bad16(v_pages))))
+        return fail(ctx, FR_ERR_INVALID_ARG, "k_new / v_new / k_pages / v_pages is NULL or not 16-byte aligned");
+    if (bad4(slots) || (reinterpret_cast<uintptr_t>(positions) & 3u))
+        return fail(ctx, FR_ERR_INVALID_ARG, "slots is NULL, or slots / positions not 4-byte aligned");
+    if ((q == nullptr) != (q_out == nullptr)) return fail(ctx, FR_ERR_INVALID_ARG, "q and q_out must both be given or both be NULL");
+    if (!aligned16(q) || !aligned16(q_out)) return fail(ctx, FR_ERR_INVALID_ARG, "q / q_out must be 16-byte aligned");
+    if (q && !positions) return fail(ctx, FR_ERR_INVALID_ARG, "q is given but no positions to rotate it to");
+    const int64_t q_bytes = (int64_t)n_tokens * ctx->shape.Hq * ctx->shape.d * ctx->shape.esize;
+    if (q && q != q_out && (const char*)q < (const char*)q_out + q_bytes && (const char*)q_out < (const char*)q + q_bytes)
+        return fail(ctx, FR_ERR_INVALID_ARG, "q and q_out overlap without being equal");
+    if ((st = need_device(ctx)) != FR_OK) return st;
+    PagedAppendArgs a;
+    a.q = q; a.k = k_new; a.v = v_new; a.positions = positions; a.slots = slots; a.n_tokens = n_tokens;
+    a.k_pages = k_pages; a.v_pages = v_pages; a.n_rows = (int64_t)n_pages * page_rows;
+    a.q_out = q_out; a.theta = ctx->ws.rope_theta; a.Hq = ctx->shape.Hq; a.Hkv = ctx->shape.Hkv;
+    hipError_t e = launch_paged_append(ctx->shape, a, ctx->ws.n_cu, (hipStream_t)stream);
+    if (e != hipSuccess) return hip_fail(ctx, "paged append launch", e);
+    return FR_OK;
+}
+
+fr_status fr_paged_attn(fr_ctx* ctx, const void* q, const int32_t* q_offsets, const int32_t* cached_len, int32_t n_requests,
+                        int32_t n_tokens, int32_t max_new, const void* k_pages, const void* v_pages, int32_t n_pages,
+                        int32_t page_rows, const int32_t* block_table, int32_t max_blocks, void* out, float* lse_out,
+                        void* stream) {
+    if (!ctx) return FR_ERR_INVALID_ARG;
+    ctx->err.clear();
+    fr_status st = check_table(ctx, n_requests, page_rows, max_blocks);
+    if (st != FR_OK) return st;
+    if ((st = check_tokens(ctx, n_tokens)) != FR_OK) return st;
+    if ((st = check_pages(ctx, n_pages, page_rows)) != FR_OK) return st;
+    if (max_new < 0) return fail(ctx, FR_ERR_INVALID_ARG, "max_new = %d is negative", max_new);
+    if (n_tokens == 0 || n_requests == 0 || max_new == 0) return FR_OK;
+    if (bad16(q) || bad16(out) || (n_pages > 0 && (bad16(k_pages) || bad16(v_pages))))
+        return fail(ctx, FR_ERR_INVALID_ARG, "q / out / k_pages / v_pages is NULL or not 16-byte aligned");
+    if (bad4(q_offsets) || bad4(cached_len) || (max_blocks > 0 && bad4(block_table)))
+        return fail(ctx, FR_ERR_INVALID_ARG, "q_offsets / cached_len / block_table is NULL or not 4-byte aligned");
+    if (reinterpret_cast<uintptr_t>(lse_out) & 3u) return fail(ctx, FR_ERR_INVALID_ARG, "lse_out must be 4-byte aligned");
+    if ((st = need_device(ctx)) != FR_OK) return st;
+    PagedAttnArgs a{};
+    a.q = q; a.q_offsets = q_offsets; a.cached_len = cached_len; a.n_requests = n_requests; a.n_tokens = n_tokens;
+    a.max_new = max_new < n_tokens ? max_new : n_tokens;
+    a.k_pages = k_pages; a.v_pages = v_pages; a.n_pages = n_pages; a.page_rows = page_rows;
+    a.block_table = block_table; a.max_blocks = max_blocks; a.out = out; a.lse = lse_out;
+    hipError_t e = launch_paged_attn(ctx->shape, a, (hipStream_t)stream);
+    if (e != hipSuccess) return hip_fail(ctx, "paged attention launch", e);
+    return FR_OK;
+}
+
 // ---- model steps around the path -------------------------------------------------------------------
 
 static fr_status check_stack(fr_ctx* ctx, const char* what) {

@@ -181,6 +181,30 @@ size_t decode_partials_bytes(const Shape& s);
 hipError_t launch_decode_attn(const Shape& s, const DecodeArgs& a, float* partials, const double* theta, int n_cu, hipStream_t st);
 hipError_t launch_mark_stale(uint32_t* bits, int64_t n_words, const int32_t* rows, int n_rows, int clear, hipStream_t st);
 
+// A serving step over a paged cache (all pointers device memory; see fr_page_tables, fr_paged_append and fr_paged_attn in the public header).
+constexpr int64_t PAGED_MAX_POSITIONS = (int64_t)1 << 30;   // of a request, and rows of a step
+struct PageTablesArgs {
+    const int32_t *cached_len, *new_len; int n_requests, page_rows;
+    const int32_t* free_pages; int n_free; const int32_t* free_start;
+    int32_t* block_table; int max_blocks, n_tokens;
+    int32_t *q_offsets, *positions, *slots, *pages_needed;
+};
+hipError_t launch_page_tables(const PageTablesArgs& a, hipStream_t st);
+struct PagedAppendArgs {
+    const void *q, *k, *v; const int32_t *positions, *slots; int n_tokens;
+    void *k_pages, *v_pages; int64_t n_rows;   // rows of the cache: pages x rows of a page
+    void* q_out; const double* theta; int Hq, Hkv;
+};
+hipError_t launch_paged_append(const Shape& s, const PagedAppendArgs& a, int n_cu, hipStream_t st);
+struct PagedAttnArgs {
+    const void* q; const int32_t *q_offsets, *cached_len; int n_requests, n_tokens, max_new;
+    const void *k_pages, *v_pages; int n_pages, page_rows;
+    const int32_t* block_table; int max_blocks;
+    void* out; float* lse;
+    int Hq, Hkv, G; float scale_log2e;   // (filled in by launch_paged_attn)
+};
+hipError_t launch_paged_attn(const Shape& s, const PagedAttnArgs& a, hipStream_t st);
+
 // When given to launch_attn_mfma, k_cache / v_cache are a chunk store shared between queries: prompt position
 // j in [ct.off[c], ct.off[c+1]) reads store row store_row0[c] + j - ct.off[c], its key rotated by deltas->delta[c]
 // positions; the launch leaves the chunks' (cos, sin) rows in `table` (device scratch, [chunks][d/2]).  store_row0 and

@@ -82,3 +82,71 @@ class SelectivePrefillStack:
             if capture is not None and l in capture:
                 capture[l]["h_out"] = h.clone()
         return h
+
+
+class PagedCache:
+    """K/V of up to `n_requests` requests in pages of `page_rows` rows, for every layer; one free list and one block table serve all layers.
+    Lengths and tables stay on the device (a captured step serves other lengths)."""
+
+    def __init__(self, n_layers: int, n_requests: int, n_pages: int, page_rows: int, max_blocks: int, Hkv: int, d: int,
+                 dtype=torch.bfloat16):
+        i32 = dict(dtype=torch.int32, device="cuda")
+        shape = (n_pages, page_rows, Hkv, d)
+        self.k = [torch.zeros(shape, dtype=dtype, device="cuda") for _ in range(n_layers)]
+        self.v = [torch.zeros(shape, dtype=dtype, device="cuda") for _ in range(n_layers)]
+        self.n_requests, self.n_pages, self.page_rows, self.max_blocks = n_requests, n_pages, page_rows, max_blocks
+        self.block_table = torch.full((n_requests, max_blocks), -1, **i32)
+        self.cached_len = torch.zeros(n_requests, **i32)
+        self.free_pages = torch.arange(n_pages, **i32)
+        self.free_start, self.pages_needed = torch.zeros(1, **i32), torch.zeros(1, **i32)
+
+
+class PagedStack:
+    """Decoder layers over a paged cache: a step appends new_len[b] rows to every request b (a decoding step, drafted tokens, a chunk of
+    a prompt, a whole prompt, side by side) and computes them.  Per layer: RMSNorm, Q/K/V projection with each row's own position,
+    fr_paged_append, fr_paged_attn, output projection and feed-forward."""
+
+    def __init__(self, ctx: B.Context, layers: List[LayerWeights], hidden: int, ffn: int, eps: float = 1e-5):
+        self.ctx, self.layers, self.hidden, self.ffn, self.eps = ctx, layers, hidden, ffn, eps
+        d = ctx.desc
+        self.Hq, self.Hkv, self.d = d.n_q_heads, d.n_kv_heads, d.head_dim
+        # fr_qkv_rope rotates rows of this layout itself; others are projected part by part and rotated on the way into the pages
+        self.fused_rope = d.head_dim == 128 and d.rope_layout == B.FR_ROPE_INTERLEAVED
+        self._buf = {}
+
+    def _scratch(self, T: int, n: int):
+        if self._buf.get("key") != (T, n):
+            mk = lambda *shape: torch.empty(shape, dtype=torch.bfloat16, device="cuda")
+            i32 = lambda m: torch.empty(m, dtype=torch.int32, device="cuda")
+            self._buf = dict(key=(T, n), x=mk(T, self.hidden), q=mk(T, self.Hq, self.d), k=mk(T, self.Hkv, self.d), v=mk(T, self.Hkv, self.d),
+                             attn=torch.zeros((T, self.Hq, self.d), dtype=torch.bfloat16, device="cuda"), act=mk(T, self.ffn),
+                             offsets=i32(n + 1), positions=i32(T), slots=i32(T))
+        return self._buf
+
+    def forward(self, h: torch.Tensor, new_len: torch.Tensor, max_new: int, cache: PagedCache) -> torch.Tensor:
+        """h [T, hidden] is updated in place and returned: the requests' rows one after the other, rows behind them hold nothing of use.
+        new_len [n_requests] int32 on the device, none beyond max_new.  The cache's lengths and free list move on."""
+        c, T, n = self.ctx, h.shape[0], cache.n_requests
+        s = self._scratch(T, n)
+        c.fr_page_tables(cache.cached_len, new_len, n, cache.page_rows, cache.free_pages, cache.n_pages, cache.free_start, cache.block_table,
+                         cache.max_blocks, T, s["offsets"], s["positions"], s["slots"], cache.pages_needed)
+        nq, nk = self.Hq * self.d, self.Hkv * self.d
+        for l, w in enumerate(self.layers):
+            kp, vp = cache.k[l], cache.v[l]
+            c.fr_rmsnorm(h, w.g1, T, self.hidden, self.eps, s["x"])
+            if self.fused_rope:
+                c.fr_qkv_rope(s["x"], w.w_qkv, T, self.hidden, s["positions"], s["q"], s["k"], s["v"])
+                c.fr_paged_append(None, s["k"], s["v"], None, s["slots"], T, kp, vp, cache.n_pages, cache.page_rows)
+            else:
+                for out, at, rows in ((s["q"], 0, nq), (s["k"], nq, nk), (s["v"], nq + nk, nk)):
+                    c.fr_linear(s["x"], w.w_qkv[at: at + rows], T, rows, self.hidden, None, out)
+                c.fr_paged_append(s["q"], s["k"], s["v"], s["positions"], s["slots"], T, kp, vp, cache.n_pages, cache.page_rows, s["q"])
+            c.fr_paged_attn(s["q"], s["offsets"], cache.cached_len, n, T, max_new, kp, vp, cache.n_pages, cache.page_rows, cache.block_table,
+                            cache.max_blocks, s["attn"])
+            c.fr_linear(s["attn"], w.w_o, T, self.hidden, nq, h, h)
+            c.fr_rmsnorm(h, w.g2, T, self.hidden, self.eps, s["x"])
+            c.fr_linear_swiglu(s["x"], w.w_gate_up, T, self.ffn, self.hidden, s["act"])
+            c.fr_linear(s["act"], w.w_down, T, self.hidden, self.ffn, h, h)
+        cache.cached_len += s["offsets"][1:] - s["offsets"][:-1]
+        cache.free_start += cache.pages_needed
+        return h
