@@ -3,6 +3,7 @@
 #include <stdarg.h>
 #include <stdio.h>
 
+#include <algorithm>
 #include <new>
 
 #include "fr_internal.hpp"
@@ -151,7 +152,7 @@ fr_status fr_create(const fr_layer_desc* desc, int64_t max_tokens, int32_t max_c
     const size_t o_img = take(w.kv_images_bytes);
     w.attn_partials_bytes = tiled ? attn_mfma_partials_bytes(s, max_tokens) : 0;
     const size_t o_part = take(w.attn_partials_bytes);
-    const size_t o_dpart = take(decode_partials_bytes(s));
+    const size_t o_dpart = take(std::max(decode_partials_bytes(s), paged_attn_partials_bytes(s, w.n_cu)));
     const size_t o_theta = take((size_t)(s.d / 2) * sizeof(double));
     const size_t o_rr = take((size_t)max_tokens * (s.d / 2) * sizeof(float2));
     w.gemm_partials_bytes = (s.dtype == FR_BF16) ? gemm_partials_bytes() : 0;
@@ -932,7 +933,7 @@ fr_status fr_paged_attn(fr_ctx* ctx, const void* q, const int32_t* q_offsets, co
     a.max_new = max_new < n_tokens ? max_new : n_tokens;
     a.k_pages = k_pages; a.v_pages = v_pages; a.n_pages = n_pages; a.page_rows = page_rows;
     a.block_table = block_table; a.max_blocks = max_blocks; a.out = out; a.lse = lse_out;
-    hipError_t e = launch_paged_attn(ctx->shape, a, (hipStream_t)stream);
+    hipError_t e = launch_paged_attn(ctx->shape, a, ctx->ws.decode_partials, ctx->ws.n_cu, (hipStream_t)stream);
     if (e != hipSuccess) return hip_fail(ctx, "paged attention launch", e);
     return FR_OK;
 }

@@ -54,7 +54,7 @@ struct Workspace {
     float* gemm_partials = nullptr; // partial sums of the GEMM tiles that are split along K
     size_t gemm_partials_bytes = 0;
     float2* rope_rows = nullptr;    // [max_tokens][d/2] (cos, sin) of the recomputed rows' positions
-    float* decode_partials = nullptr;    // [DECODE_MAX_UNITS][Hq][d + 2] partial softmax results of fr_decode_attn's pieces
+    float* decode_partials = nullptr;    // partial softmax results: [DECODE_MAX_UNITS][Hq][d + 2] of fr_decode_attn's pieces, or those of fr_paged_attn
     double* rope_theta = nullptr;        // [d/2] rotary frequencies base^(-2 (p + index_base) / d)
     float* attn_partials = nullptr;      // partial results of an attention launch whose items are computed in parts
     size_t attn_partials_bytes = 0;
@@ -201,9 +201,9 @@ struct PagedAttnArgs {
     const void *k_pages, *v_pages; int n_pages, page_rows;
     const int32_t* block_table; int max_blocks;
     void* out; float* lse;
-    int Hq, Hkv, G; float scale_log2e;   // (filled in by launch_paged_attn)
 };
-hipError_t launch_paged_attn(const Shape& s, const PagedAttnArgs& a, hipStream_t st);
+size_t paged_attn_partials_bytes(const Shape& s, int n_cu);
+hipError_t launch_paged_attn(const Shape& s, const PagedAttnArgs& a, float* partials, int n_cu, hipStream_t st);
 
 // When given to launch_attn_mfma, k_cache / v_cache are a chunk store shared between queries: prompt position
 // j in [ct.off[c], ct.off[c+1]) reads store row store_row0[c] + j - ct.off[c], its key rotated by deltas->delta[c]

@@ -1,0 +1,158 @@
+// What the attention kernels over a paged cache share: their arguments, how the work of a launch is dealt out, and how pieces of an item are joined.
+#pragma once
+
+#include "fr_internal.hpp"
+
+namespace fr {
+
+// Arguments of the kernels.  A launch takes the requests with cols_lo < rows x G <= cols_hi query columns.
+struct PagedArgs {
+    const void* q;
+    const int32_t *q_offsets, *cached_len, *block_table;
+    const void *k_pages, *v_pages;
+    void* out;
+    float* lse;
+    float* partials;
+    int B, T, max_new, n_pages, P, W, cap;   // cap = W P: positions that the table has room for
+    int Hq, Hkv, G, cols_lo, cols_hi;
+    int n_wg;                // workgroups per KV head that the work is dealt to
+    uint32_t g_magic;        // ceil(2^32 / G): c / G = mulhi(c, g_magic) for c < 2^26
+    uint32_t p_magic, p_shift;   // j / P = mulhi(2 j, p_magic) >> p_shift for j < 2^30
+    float scale_log2e;
+};
+
+// A request as a launch sees it.
+struct PagedRequest {
+    int first, n;     // its first row and how many count
+    int cached;
+};
+__device__ __forceinline__ PagedRequest paged_request(const PagedArgs& a, int b) {
+    const int lo = max(min(a.q_offsets[b], a.T), 0), hi = max(min(a.q_offsets[b + 1], a.T), lo);
+    PagedRequest r;
+    r.first = lo;
+    r.n = min(hi - lo, a.max_new);
+    r.cached = a.cached_len[b];
+    const int64_t cols = (int64_t)r.n * a.G;
+    if (cols <= a.cols_lo || (a.cols_hi < INT32_MAX && cols > a.cols_hi)) r.n = 0;
+    return r;
+}
+__device__ __forceinline__ int paged_position(const PagedArgs& a, const PagedRequest& r, int i) {   // of its row i; -1: sees nothing
+    return (int)max((int64_t)-1, min((int64_t)r.cached + i, (int64_t)a.cap - 1));
+}
+__device__ __forceinline__ int paged_token(const PagedArgs& a, int col) { return a.G > 1 ? (int)__umulhi((uint32_t)col, a.g_magic) : col; }
+__device__ __forceinline__ int paged_block(const PagedArgs& a, int j) { return (int)(__umulhi(2u * (uint32_t)j, a.p_magic) >> a.p_shift); }
+
+__device__ __forceinline__ int64_t wave_sum64(int64_t v) {
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
+    return v;
+}
+__device__ __forceinline__ int64_t wave_scan64(int64_t v) {   // inclusive
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int64_t t = __shfl_up(v, d);
+        if (lane >= d) v += t;
+    }
+    return v;
+}
+__device__ __forceinline__ int64_t uniform64(int64_t v) {
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((int)(uint32_t)v), hi = __builtin_amdgcn_readfirstlane((int)(v >> 32));
+    return (int64_t)(((uint64_t)hi << 32) | lo);
+}
+
+// How a launch's work is dealt out.  The work of a KV head is one line of units: requests in order, of each its column tiles, of each its units of keys.
+// Workgroup w of n takes units floor(w U / n) .. floor((w + 1) U / n) - 1 of it, wherever they begin and end, so every workgroup has the same
+// share whatever the lengths are, and the host need not know them.  An item (column tile) that falls to several workgroups leaves a partial result
+// per piece: in slot 2 w of a workgroup whose piece begins behind the item's start, in 2 w + 1 of the one that has its start but not its end.
+struct PagedLine {
+    int64_t total;    // U
+    int64_t start;    // of the unit that was looked for: first unit of its request
+    int b;            // and the request
+};
+// cost(b) = units of request b (0: none).  Every wave does this by itself.  find(total) = the unit to look for, or -1.
+template <typename Cost, typename Find>
+__device__ __forceinline__ PagedLine paged_line(int B, Cost cost, Find find) {
+    const int lane = threadIdx.x & 63;
+    PagedLine r{0, 0, -1};
+    int64_t mine = 0;
+    for (int b0 = 0; b0 < B; b0 += 64) {
+        mine = b0 + lane < B ? cost(b0 + lane) : 0;
+        r.total += uniform64(wave_sum64(mine));
+    }
+    const int64_t u = find(r.total);
+    if (u < 0 || u >= r.total) return r;
+    for (int b0 = 0; b0 < B; b0 += 64) {
+        if (B > 64) mine = b0 + lane < B ? cost(b0 + lane) : 0;
+        const int64_t upto = r.start + wave_scan64(mine);
+        const uint64_t beyond = __ballot(upto > u);
+        if (beyond != 0) {
+            const int l = __builtin_ctzll(beyond);
+            r.b = b0 + l;
+            const int64_t end = uniform64(__shfl(upto, l)), own = uniform64(__shfl(mine, l));
+            r.start = end - own;
+            return r;
+        }
+        r.start = uniform64(__shfl(upto, 63));
+    }
+    return r;
+}
+__device__ __forceinline__ int64_t paged_first_unit(int64_t w, int64_t total, int n) { return w * total / n; }
+__device__ __forceinline__ int paged_owner(int64_t u, int64_t total, int n) { return (int)(((u + 1) * n - 1) / total); }   // the workgroup that has unit u
+
+// ---- matrix-core helpers ------------------------------------------------------------------------------
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+constexpr float PAGED_NO_MAX = -1.0e30f;   // exponent reference of a column that has seen nothing
+constexpr float PAGED_RAISE = 8.f;         // a column's reference goes up when a logit is this far (base 2) above it: weights stay below 2^8
+
+// Sum and maximum over the four lanes that hold the same column (lanes x, x + 16, x + 32, x + 48).
+__device__ __forceinline__ float paged_column_sum(float v) {
+    auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float paged_column_max(float v) {
+    auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ uint32_t paged_finite_or_zero(uint32_t w) {   // the two bf16 numbers of a word, 0 in the place of one that is not finite
+    if ((w & 0x00007F80u) == 0x00007F80u) w &= 0xFFFF0000u;
+    if ((w & 0x7F800000u) == 0x7F800000u) w &= 0x0000FFFFu;
+    return w;
+}
+__device__ __forceinline__ bool paged_not_finite(uint32_t w) { return (w & 0x00007F80u) == 0x00007F80u || (w & 0x7F800000u) == 0x7F800000u; }
+
+// ---- copies global -> LDS without registers; completion: the issuing wave's vmcnt, in order of issue ------
+__device__ __forceinline__ uint32_t paged_lds(const void* p) {
+    return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) const unsigned char*)p);
+}
+__device__ __forceinline__ void paged_copy16(const void* src, uint32_t lds) {   // lane i's 16 bytes to lds + 16 i
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(src), "s"(lds) : "memory");
+}
+__device__ __forceinline__ void paged_copy4(const void* src, uint32_t lds) {    // lane i's 4 bytes to lds + 4 i
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(src), "s"(lds) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void paged_wait_but() {   // until all but the wave's last N copies have landed
+    static_assert(N < 16, "one field of the counter");
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0f70 | N);
+    asm volatile("" ::: "memory");
+}
+
+size_t paged_stream_partials_bytes(const Shape& s, int n_cu);
+hipError_t launch_paged_stream(const Shape& s, const PagedArgs& a, int n_cu, hipStream_t st);
+
+// ---- joining pieces -----------------------------------------------------------------------------------
+// A piece's slot: [column][D + 2] fp32: exponent reference (base 2), sum of weights, weighted values.
+template <int D>
+constexpr int paged_part_floats() { return D + 2; }
+
+}  // namespace fr

@@ -3,7 +3,7 @@
 //
 // One workgroup per (row, KV head), four query heads at a time: a group of lanes per key row, 16 bytes each, an online softmax per lane group,
 // merged through LDS at the end.
-#include "fr_internal.hpp"
+#include "k_paged.hpp"
 
 #include <algorithm>
 
@@ -15,18 +15,17 @@ constexpr float NEG_BIG = -1.0e30f;
 constexpr int GC = 4;
 
 template <typename T, int D>
-__global__ __launch_bounds__(256) void paged_rows_kernel(const PagedAttnArgs a) {
+__global__ __launch_bounds__(256) void paged_rows_kernel(const PagedArgs a) {
     constexpr int N = 16 / sizeof(T), LPK = D / N, KPW = 64 / LPK;
     __shared__ float mo[4][GC][D], mm[4][GC], ml[4][GC];
     const int t = blockIdx.x, g = blockIdx.y, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, c = lane % LPK, r = lane / LPK;
     int b = -1, first = 0;
-    for (int i = 0; i < a.n_requests; ++i) {
-        const int lo = max(a.q_offsets[i], 0), hi = min(a.q_offsets[i + 1], a.n_tokens);
-        if (t >= lo && t < hi) { b = i; first = lo; break; }
+    for (int i = 0; i < a.B; ++i) {
+        const PagedRequest r = paged_request(a, i);
+        if (t >= r.first && t < r.first + r.n) { b = i; first = r.first; break; }
     }
-    if (b < 0 || t - first >= a.max_new) return;
-    const int64_t cap = (int64_t)a.max_blocks * a.page_rows;
-    const int seen = (int)min((int64_t)a.cached_len[b] + (t - first) + 1, cap);   // keys 0 .. seen - 1
+    if (b < 0) return;
+    const int seen = paged_position(a, paged_request(a, b), t - first) + 1;   // keys 0 .. seen - 1
     for (int h0 = 0; h0 < a.G; h0 += GC) {
         float q[GC][N], o[GC][N], m[GC], l[GC];
 #pragma unroll
@@ -38,9 +37,9 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(const PagedAttnArgs a) 
         }
         for (int j0 = 0; j0 < seen; j0 += 4 * KPW) {
             const int j = j0 + wave * KPW + r;
-            const int page = j < seen ? a.block_table[(size_t)b * a.max_blocks + j / a.page_rows] : -1;
+            const int page = j < seen ? a.block_table[(size_t)b * a.W + paged_block(a, j)] : -1;
             const bool ok = page >= 0 && page < a.n_pages;
-            const size_t at = ok ? (((size_t)page * a.page_rows + j % a.page_rows) * a.Hkv + g) * D + c * N : 0;
+            const size_t at = ok ? (((size_t)page * a.P + (j - paged_block(a, j) * a.P)) * a.Hkv + g) * D + c * N : 0;
             float kf[N], vf[N];
 #pragma unroll
             for (int e = 0; e < N; ++e) {
@@ -96,20 +95,41 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(const PagedAttnArgs a) 
 }
 
 template <typename T, int D>
-hipError_t launch(const PagedAttnArgs& a, hipStream_t st) {
-    paged_rows_kernel<T, D><<<dim3((unsigned)a.n_tokens, (unsigned)a.Hkv), dim3(256), 0, st>>>(a);
+hipError_t launch_rows(const PagedArgs& a, hipStream_t st) {
+    paged_rows_kernel<T, D><<<dim3((unsigned)a.T, (unsigned)a.Hkv), dim3(256), 0, st>>>(a);
     return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_paged_attn(const Shape& s, const PagedAttnArgs& args, hipStream_t st) {
+hipError_t launch_paged_attn(const Shape& s, const PagedAttnArgs& args, float* partials, int n_cu, hipStream_t st) {
     if (args.n_tokens == 0 || args.n_requests == 0 || args.max_new == 0) return hipSuccess;
-    PagedAttnArgs a = args;
+    PagedArgs a{};
+    a.q = args.q; a.q_offsets = args.q_offsets; a.cached_len = args.cached_len; a.block_table = args.block_table;
+    a.k_pages = args.k_pages; a.v_pages = args.v_pages; a.out = args.out; a.lse = args.lse; a.partials = partials;
+    a.B = args.n_requests; a.T = args.n_tokens; a.max_new = args.max_new;
+    a.n_pages = args.n_pages; a.P = args.page_rows; a.W = args.max_blocks;
+    a.cap = args.n_pages > 0 ? args.max_blocks * args.page_rows : 0;   // (a cache without pages shows nothing)
     a.Hq = s.Hq; a.Hkv = s.Hkv; a.G = s.G;
+    a.g_magic = (uint32_t)((((uint64_t)1 << 32) + s.G - 1) / s.G);
+    while (((int64_t)1 << a.p_shift) < a.P) ++a.p_shift;
+    a.p_magic = (uint32_t)(2 * ((((uint64_t)1 << (30 + a.p_shift)) + a.P - 1) / a.P));
     a.scale_log2e = (1.0f / sqrtf((float)s.d)) * 1.4426950408889634f;
-    if (s.dtype == FR_BF16) return s.d == 128 ? launch<__bf16, 128>(a, st) : launch<__bf16, 64>(a, st);
-    return s.d == 128 ? launch<float, 128>(a, st) : launch<float, 64>(a, st);
+    if (s.dtype != FR_BF16) {
+        a.cols_hi = INT32_MAX;
+        return s.d == 128 ? launch_rows<float, 128>(a, st) : launch_rows<float, 64>(a, st);
+    }
+    // requests with few columns, and the others
+    const int few = std::max(64, s.G);
+    a.cols_lo = 0;
+    a.cols_hi = few;
+    hipError_t e = launch_paged_stream(s, a, n_cu, st);
+    if (e != hipSuccess || (int64_t)args.max_new * s.G <= few) return e;
+    a.cols_lo = few;
+    a.cols_hi = INT32_MAX;
+    return s.d == 128 ? launch_rows<__bf16, 128>(a, st) : launch_rows<__bf16, 64>(a, st);
 }
+
+size_t paged_attn_partials_bytes(const Shape& s, int n_cu) { return s.dtype == FR_BF16 ? paged_stream_partials_bytes(s, n_cu) : 0; }
 
 }  // namespace fr

@@ -1,0 +1,468 @@
+// Attention over a paged cache, requests with few query columns (decoding, drafted tokens): bf16, head_dim 64 or 128.
+//
+// Every byte of K and V is used for a handful of columns, so the rate of memory is the bound.  One workgroup = one KV head x 16 NC query columns
+// ((row, query head) pairs, the heads of the group fastest); its four waves deal the blocks of 32 keys among themselves, each with accumulators of its own
+// that are merged through LDS at the end of a piece: nothing in the loop waits for another wave.  The line of work is dealt out in equal shares
+// (k_paged.hpp).
+//
+// S^T = K Q^T and O^T = V^T P^T with v_mfma_f32_16x16x32_bf16, keys on the register dimension of S^T and columns on lanes: the accumulators of two 16-key
+// blocks are, after conversion, the B operand of the second product.  Row m of value product md is dim D / 16 m + md, so that a lane needs 16 (8)
+// neighbouring bytes of each of its eight value rows and transposes them itself with byte permutes.  Weights go into the second product as bf16 (half a
+// step, 2^-8, of each; their sum is taken in fp32 before), as the output does.
+//
+// A wave copies a block global -> LDS (no registers, no wait) while it works on the one before.  The page numbers of a block's keys come the same way
+// one block earlier, so that the copies of a wave are the only thing its memory counter counts, and every page size goes the same way.
+//
+// Softmax.  A column's exponent reference goes up, and its sums are scaled, only when a logit is 8 (base 2) or more above it.
+//
+// What a column does not see stays out of it by hand, as a weight of 0 does not take a NaN or an infinity out of a product: keys behind the tile's last
+// row repeat that one, and values that are not finite leave a block that only some columns see whole and reach those columns when the loop is over.
+#include "k_paged.hpp"
+
+#include <algorithm>
+
+namespace fr {
+
+namespace {
+
+constexpr int W = 4;              // waves per workgroup
+constexpr int UNIT = 32 * W;      // keys of a unit of work: a block for every wave
+
+template <int D, int NC>
+struct StreamLds {
+    static constexpr int TILE = 32 * D * 2;   // bytes of a block of 32 keys or values
+    static constexpr int C = 16 * NC;
+    int32_t page[W][2][64];                   // page numbers of the keys of a wave's next blocks
+    union {
+        struct { unsigned char k[W][TILE], v[W][TILE]; };
+        struct {
+            float o[W][C][D + 4];
+            float m[C][W], l[C][W];
+        };
+    };
+};
+
+// Units of a request: column tiles x units of keys.
+template <int C>
+__device__ __forceinline__ int64_t stream_cost(const PagedArgs& a, int b, int* n_ct = nullptr, int* n_units = nullptr, PagedRequest* req = nullptr) {
+    const PagedRequest r = paged_request(a, b);
+    if (req) *req = r;
+    if (r.n == 0) return 0;
+    const int ct = (r.n * a.G + C - 1) / C, units = max(paged_position(a, r, r.n - 1), 0) / UNIT + 1;
+    if (n_ct) { *n_ct = ct; *n_units = units; }
+    return (int64_t)ct * units;
+}
+
+template <int D, int NC, bool ALIGNED>
+struct StreamPiece {
+    static constexpr int NJ = D / 16, NK = D / 32, VW = D / 32;   // dims per lane of a value row, matrix steps of a logit, words of a lane's values
+    static constexpr int RV = D / 8, COPIES = 32 * RV / 64;       // vectors of a row; copies of 1 KB of a block
+    static constexpr int C = 16 * NC;
+    using Lds = StreamLds<D, NC>;
+    typedef __attribute__((ext_vector_type(VW))) uint32_t VVec;
+
+    // One piece: units [r0, r1) of column tile ct of request b.  whole: it is all of the item, the outputs are stored; else the partial result goes to `part`.
+    static __device__ __forceinline__ void run(const PagedArgs& a, Lds& sm, const PagedRequest& rq, int b, int ct, int g, int r0, int r1, bool whole, float* part) {
+        const int tid = threadIdx.x, lane = tid & 63, x = lane & 15, kg = lane >> 4;
+        const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+        const int G = a.G, cols = rq.n * G, col0 = C * ct;
+        const __bf16* q_rows = (const __bf16*)a.q;
+        auto out_row = [&](int col) {   // (row, head) of a column, counted over all heads
+            const int i = paged_token(a, col);
+            return (size_t)(rq.first + i) * a.Hq + g * G + (col - i * G);
+        };
+        bf16x8 qf[NC][NK];   // B operand of S^T = K Q^T
+        int pos[NC];
+#pragma unroll
+        for (int nb = 0; nb < NC; ++nb) {   // columns past the end: a copy of the last
+            const int n = min(col0 + 16 * nb + x, cols - 1);
+            const __bf16* p = q_rows + out_row(n) * D + 8 * kg;
+            pos[nb] = paged_position(a, rq, paged_token(a, n));
+#pragma unroll
+            for (int ks = 0; ks < NK; ++ks) qf[nb][ks] = *reinterpret_cast<const bf16x8*>(p + 32 * ks);
+        }
+        const int p_first = paged_position(a, rq, paged_token(a, col0));                          // keys up to here are visible to every column
+        const int p_last = paged_position(a, rq, paged_token(a, min(col0 + C, cols) - 1));
+        const int n_blocks = min((p_last + 32) / 32, W * r1);                                     // (none for a tile that sees nothing)
+        f32x4 o[NJ][NC];   // O^T: row m of product md is dim NJ m + md
+        float m[NC], l[NC];
+#pragma unroll
+        for (int nb = 0; nb < NC; ++nb) {
+            m[nb] = PAGED_NO_MAX;
+            l[nb] = 0.f;
+#pragma unroll
+            for (int md = 0; md < NJ; ++md) o[md][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+        const int32_t* table = a.block_table + (size_t)b * a.W;
+        const uint32_t row_bytes = (uint32_t)(a.Hkv * D * 2);
+        const unsigned char *k_base = (const unsigned char*)a.k_pages + (size_t)g * D * 2, *v_base = (const unsigned char*)a.v_pages + (size_t)g * D * 2;
+        // A copy brings 64 / RV rows, RV lanes side by side to a row; copy i the rows COPIES q + i of the lanes' groups q, so that a lane's sources are
+        // neighbours.  Vector c of key row r sits in place c ^ swz(r), so that the 16 rows of a fragment read meet in no bank.
+        auto swz = [](int r) { return D == 128 ? r & 15 : (r & 3) | (r >> 1 & 4); };
+        auto row_at = [](int r) { return 1024 * (r % COPIES) + 16 * RV * (r / COPIES); };
+        const uint32_t k_lds = paged_lds(sm.k[wave]), v_lds = paged_lds(sm.v[wave]), page_lds = paged_lds(sm.page[wave]);
+        const int qg = lane / RV, vec = lane % RV;
+        const uint32_t k_place = 16 * (vec ^ swz(COPIES * qg)), v_place = 16 * vec;   // swz(COPIES q + i) = swz(COPIES q) ^ swz(i)
+        auto is_page = [&](int p) { return (uint32_t)p < (uint32_t)a.n_pages; };
+        auto copy_pages = [&](int blk, int ring) {   // of keys 32 blk .. 32 blk + 31 (twice)
+            paged_copy4(table + paged_block(a, min(32 * blk + (lane & 31), p_last)), page_lds + 256 * ring);
+        };
+        uint32_t row[COPIES];   // cache rows of the lane's keys of the block on its way
+        bool holes_next = false;
+        auto find_rows = [&](int blk, int ring) {
+            const int j0 = 32 * blk + COPIES * qg;
+            bool hole = false;
+            if constexpr (ALIGNED) {   // pages are whole multiples of the lane's COPIES rows
+                const int page = sm.page[wave][ring][COPIES * qg], jc = min(j0, p_last), in = j0 - jc, base = jc - paged_block(a, jc) * a.P;
+                hole = !is_page(page);
+                const uint32_t at = (uint32_t)(hole ? 0 : page) * (uint32_t)a.P + (uint32_t)base;
+                const int most = p_last - jc;
+#pragma unroll
+                for (int i = 0; i < COPIES; ++i) row[i] = at + (uint32_t)min(in + i, most);
+            } else {
+#pragma unroll
+                for (int i = 0; i < COPIES; ++i) {
+                    const int page = sm.page[wave][ring][COPIES * qg + i], j = min(j0 + i, p_last);
+                    const bool none = !is_page(page);
+                    hole = hole || none;
+                    row[i] = (uint32_t)(none ? 0 : page) * (uint32_t)a.P + (uint32_t)(j - paged_block(a, j) * a.P);
+                }
+            }
+            holes_next = __any(hole);
+        };
+        auto copy_k = [&] {
+#pragma unroll
+            for (int i = 0; i < COPIES; ++i) paged_copy16(k_base + (size_t)row[i] * row_bytes + (k_place ^ (swz(i) * 16u)), k_lds + 1024 * i);
+        };
+        auto copy_v = [&] {
+#pragma unroll
+            for (int i = 0; i < COPIES; ++i) paged_copy16(v_base + (size_t)row[i] * row_bytes + v_place, v_lds + 1024 * i);
+        };
+        bool apart = false;
+        int blk = W * r0 + wave;
+        if (blk < n_blocks) {
+            const int last = n_blocks - 1;   // (past the last block: that one again, nobody uses it; the counts of the waits stay the same)
+            paged_wait_but<0>();   // (nothing that the compiler counts is in flight from here on)
+            copy_pages(blk, 0);
+            copy_pages(min(blk + W, last), 1);
+            paged_wait_but<1>();
+            find_rows(blk, 0);
+            copy_k();
+            copy_v();
+            int ring = 1;   // of the next block's pages
+#pragma unroll 1
+            for (; blk < n_blocks; blk += W) {
+                const bool holes = holes_next;
+                f32x4 s[2][NC];
+                paged_wait_but<COPIES>();   // this block's keys, and the next one's pages
+                {
+                    bf16x8 kf[2][NK];   // keys 32 blk + 16 bb + x: dims 32 ks + 8 kg ..
+#pragma unroll
+                    for (int ks = 0; ks < NK; ++ks)
+#pragma unroll
+                        for (int bb = 0; bb < 2; ++bb)
+                            kf[bb][ks] = *reinterpret_cast<const bf16x8*>(sm.k[wave] + row_at(16 * bb + x) + 16 * ((4 * ks + kg) ^ swz(x)));
+#pragma unroll
+                    for (int ks = 0; ks < NK; ++ks)
+#pragma unroll
+                        for (int bb = 0; bb < 2; ++bb)
+#pragma unroll
+                            for (int nb = 0; nb < NC; ++nb)
+                                s[bb][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[bb][ks], qf[nb][ks], ks == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[bb][nb], 0, 0, 0);
+                }
+                int hole_of[2] = {0, 0};   // bit v: key 16 bb + 4 kg + v of this block has no page
+                if (__builtin_expect(holes, 0)) {
+#pragma unroll
+                    for (int bb = 0; bb < 2; ++bb)
+#pragma unroll
+                        for (int v = 0; v < 4; ++v) hole_of[bb] |= is_page(sm.page[wave][ring ^ 1][16 * bb + 4 * kg + v]) ? 0 : 1 << v;
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                find_rows(min(blk + W, last), ring);
+                asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");   // (this block's pages and keys have been read)
+                copy_k();
+                copy_pages(min(blk + 2 * W, last), ring ^ 1);
+                ring ^= 1;
+                const bool partial = 32 * blk + 31 > p_first || holes;   // not every column sees all of these keys
+                if (partial) {
+#pragma unroll
+                    for (int bb = 0; bb < 2; ++bb)
+#pragma unroll
+                        for (int v = 0; v < 4; ++v)
+#pragma unroll
+                            for (int nb = 0; nb < NC; ++nb)
+                                if (32 * blk + 16 * bb + 4 * kg + v > pos[nb] || (hole_of[bb] >> v & 1)) s[bb][nb][v] = -INFINITY;
+                }
+                float top[NC];
+                bool raise = false;
+#pragma unroll
+                for (int nb = 0; nb < NC; ++nb) {
+                    float t = s[0][nb][0];
+#pragma unroll
+                    for (int v = 1; v < 8; ++v) t = fmaxf(t, s[v / 4][nb][v % 4]);
+                    top[nb] = paged_column_max(t) * a.scale_log2e;
+                    raise = raise || top[nb] > m[nb] + PAGED_RAISE;
+                }
+                if (__any(raise)) {
+#pragma unroll
+                    for (int nb = 0; nb < NC; ++nb) {
+                        const float up = fmaxf(m[nb], top[nb]), down = __builtin_amdgcn_exp2f(m[nb] - up);
+                        m[nb] = up;
+                        l[nb] *= down;
+#pragma unroll
+                        for (int md = 0; md < NJ; ++md) o[md][nb] *= down;
+                    }
+                }
+                u32x4 p[NC];   // weights as the B operand of the second product: slot 4 bb + v of quarter kg is key 16 bb + 4 kg + v
+#pragma unroll
+                for (int nb = 0; nb < NC; ++nb)
+#pragma unroll
+                    for (int bb = 0; bb < 2; ++bb)
+#pragma unroll
+                        for (int v = 0; v < 4; v += 2) {
+                            const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[bb][nb][v], a.scale_log2e, -m[nb]));
+                            const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[bb][nb][v + 1], a.scale_log2e, -m[nb]));
+                            l[nb] += p0 + p1;
+                            bf16x2 t;
+                            t[0] = (__bf16)p0;
+                            t[1] = (__bf16)p1;
+                            p[nb][2 * bb + v / 2] = __builtin_bit_cast(uint32_t, t);
+                        }
+                paged_wait_but<COPIES + 1>();   // this block's values
+                VVec vf[8];   // values of keys 32 blk + 16 (i / 4) + 4 kg + i % 4, dims NJ x ..
+#pragma unroll
+                for (int i = 0; i < 8; ++i) vf[i] = *reinterpret_cast<const VVec*>(sm.v[wave] + row_at(16 * (i >> 2) + 4 * kg + (i & 3)) + 2 * NJ * x);
+                if (partial) {
+                    bool bad = false;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+#pragma unroll
+                        for (int e = 0; e < VW; ++e) bad = bad || paged_not_finite(vf[i][e]);
+                    if (__builtin_expect(__any(bad), 0)) {   // values that are not finite: not into the product
+                        apart = true;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+#pragma unroll
+                            for (int e = 0; e < VW; ++e) vf[i][e] = paged_finite_or_zero(vf[i][e]);
+                    }
+                }
+#pragma unroll
+                for (int md = 0; md < NJ; ++md) {
+                    u32x4 vt;   // dim NJ x + md of the eight keys
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        vt[j] = __builtin_amdgcn_perm(vf[2 * j + 1][md / 2], vf[2 * j][md / 2], md % 2 == 0 ? 0x05040100u : 0x07060302u);
+#pragma unroll
+                    for (int nb = 0; nb < NC; ++nb)
+                        o[md][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vt), __builtin_bit_cast(bf16x8, p[nb]), o[md][nb], 0, 0, 0);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");   // (the values have been read)
+                copy_v();
+            }
+            paged_wait_but<0>();
+        }
+        if (__builtin_expect(apart, 0)) {   // the values that were left out reach the columns that see them
+#pragma unroll 1
+            for (int at = W * r0 + wave; at < n_blocks; at += W)
+#pragma unroll 1
+                for (int t = 0; t < 32; ++t) {
+                    const int j = 32 * at + t;
+                    if (j > p_last) break;
+                    const int blk0 = 32 * at, page_block = paged_block(a, j), page = table[page_block];
+                    if (!is_page(page)) continue;
+                    // (only what the loop left out: blocks that some column does not see whole)
+                    bool partial = blk0 + 31 > p_first;
+                    if (!partial) {
+                        for (int i = 0; i < 32; ++i) partial = partial || !is_page(table[paged_block(a, blk0 + i)]);
+                    }
+                    if (!partial) continue;
+                    const uint16_t* key = (const uint16_t*)(v_base + ((size_t)page * a.P + (j - page_block * a.P)) * row_bytes);
+#pragma unroll
+                    for (int v = 0; v < 4; ++v)
+#pragma unroll
+                        for (int md = 0; md < NJ; ++md) {
+                            const uint32_t w = key[NJ * (4 * kg + v) + md];
+                            const float add = (w & 0x7F80u) == 0x7F80u ? __uint_as_float(w << 16) : 0.f;
+#pragma unroll
+                            for (int nb = 0; nb < NC; ++nb) o[md][nb][v] += j <= pos[nb] ? add : 0.f;
+                        }
+                }
+        }
+        __syncthreads();   // everyone is done with the copies
+        // ---- merge the waves ---------------------------------------------------------------------------------------------
+#pragma unroll
+        for (int nb = 0; nb < NC; ++nb) {
+            const float sum = paged_column_sum(l[nb]);
+            if (kg == 0) { sm.m[16 * nb + x][wave] = m[nb]; sm.l[16 * nb + x][wave] = sum; }
+#pragma unroll
+            for (int v = 0; v < 4; ++v)
+#pragma unroll
+                for (int h = 0; h < NJ / 4; ++h)
+                    *reinterpret_cast<f32x4*>(&sm.o[wave][16 * nb + x][NJ * (4 * kg + v) + 4 * h]) =
+                        f32x4{o[4 * h][nb][v], o[4 * h + 1][nb][v], o[4 * h + 2][nb][v], o[4 * h + 3][nb][v]};
+        }
+        __syncthreads();
+        constexpr int NV = D / 8;
+        for (int i = tid; i < C * NV; i += 64 * W) {
+            const int c = i / NV, v8 = i % NV, n = col0 + c;
+            if (n >= cols) break;
+            float mw[W], lsum = 0.f, top = PAGED_NO_MAX;
+#pragma unroll
+            for (int w = 0; w < W; ++w) { mw[w] = sm.m[c][w]; top = fmaxf(top, mw[w]); }
+            f32x4 lo = {0.f, 0.f, 0.f, 0.f}, hi = lo;
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                const float f = __builtin_amdgcn_exp2f(mw[w] - top);   // (a wave that saw nothing: 0, beside one that did)
+                lsum = __builtin_fmaf(sm.l[c][w], f, lsum);
+                lo += *reinterpret_cast<const f32x4*>(&sm.o[w][c][8 * v8]) * f;
+                hi += *reinterpret_cast<const f32x4*>(&sm.o[w][c][8 * v8 + 4]) * f;
+            }
+            if (!whole) {
+                float* dst = part + c * paged_part_floats<D>();
+                if (v8 == 0) { dst[0] = top; dst[1] = lsum; }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) { dst[2 + 8 * v8 + e] = lo[e]; dst[6 + 8 * v8 + e] = hi[e]; }
+                continue;
+            }
+            const bool none = lsum == 0.f;   // it saw nothing (the largest weight of one that did is at least 2^-8)
+            const float inv_l = none ? 0.f : 1.0f / lsum;
+            struct alignas(16) { __bf16 v[8]; } y;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                y.v[e] = (__bf16)(lo[e] * inv_l);
+                y.v[4 + e] = (__bf16)(hi[e] * inv_l);
+            }
+            const size_t oc = out_row(n);
+            *reinterpret_cast<u32x4*>((__bf16*)a.out + oc * D + 8 * v8) = __builtin_bit_cast(u32x4, y);
+            if (v8 == 0 && a.lse != nullptr) a.lse[oc] = none ? -INFINITY : (top + __builtin_amdgcn_logf(lsum)) * 0.6931471805599453f;
+        }
+        __syncthreads();   // (the next piece's copies overwrite what was merged)
+    }
+};
+
+// blockIdx.x = workgroup w of the KV head x Hkv + KV head.
+template <int D, int NC, bool ALIGNED>
+__global__ __launch_bounds__(64 * W, 2) void paged_stream_kernel(const PagedArgs a) {
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem_raw[];
+    auto& sm = *reinterpret_cast<StreamLds<D, NC>*>(smem_raw);
+    constexpr int C = 16 * NC;
+    const int g = blockIdx.x % a.Hkv, w = blockIdx.x / a.Hkv;
+    int64_t u = 0, end = 0;
+    const PagedLine line = paged_line(a.B, [&](int b) { return stream_cost<C>(a, b); }, [&](int64_t total) {
+        u = paged_first_unit(w, total, a.n_wg);
+        end = paged_first_unit(w + 1, total, a.n_wg);
+        return u < end ? u : -1;
+    });
+    if (line.b < 0) return;
+    int64_t start = line.start;   // of the request's units
+    for (int b = line.b; u < end && b < a.B; ++b) {
+        int n_ct, units;
+        PagedRequest rq;
+        const int64_t cost = stream_cost<C>(a, b, &n_ct, &units, &rq);
+        if (cost == 0) continue;
+        while (u < end && u < start + cost) {
+            const int64_t in = u - start;
+            const int ct = (int)(in / units), r0 = (int)(in - (int64_t)ct * units);
+            const int r1 = (int)min((int64_t)units, r0 + (end - u));
+            const bool whole = r0 == 0 && r1 == units;
+            float* part = a.partials + ((size_t)blockIdx.x * 2 + (r0 > 0 ? 0 : 1)) * (C * paged_part_floats<D>());
+            StreamPiece<D, NC, ALIGNED>::run(a, sm, rq, b, ct, g, r0, r1, whole, part);
+            u += r1 - r0;
+        }
+        start += cost;
+    }
+}
+
+// One workgroup per (request, column tile, KV head): joins the pieces of an item that fell to several workgroups, in their order.
+template <int D, int NC>
+__global__ __launch_bounds__(256) void paged_stream_join_kernel(const PagedArgs a, int max_ct) {
+    constexpr int C = 16 * NC, PF = paged_part_floats<D>();
+    const int g = blockIdx.x % a.Hkv, ct = blockIdx.x / a.Hkv % max_ct, b = blockIdx.x / a.Hkv / max_ct;
+    int n_ct, units;
+    PagedRequest rq;
+    const int64_t cost = stream_cost<C>(a, b, &n_ct, &units, &rq);
+    if (cost == 0 || ct >= n_ct) return;
+    int64_t before = 0, all = 0;
+    const int lane = threadIdx.x & 63;
+    for (int b0 = 0; b0 < a.B; b0 += 64) {
+        const int64_t c = b0 + lane < a.B ? stream_cost<C>(a, b0 + lane) : 0;
+        all += uniform64(wave_sum64(c));
+        before += uniform64(wave_sum64(b0 + lane < b ? c : 0));
+    }
+    const int64_t u0 = before + (int64_t)ct * units;
+    const int w0 = paged_owner(u0, all, a.n_wg), w1 = paged_owner(u0 + units - 1, all, a.n_wg);
+    if (w0 == w1) return;   // whole: stored already
+    const int cols = min(C, rq.n * a.G - C * ct), n = w1 - w0 + 1;
+    auto piece = [&](int i) { return a.partials + (((size_t)(w0 + i) * a.Hkv + g) * 2 + (i == 0 ? 1 : 0)) * (C * PF); };
+    for (int idx = threadIdx.x; idx < cols * D; idx += 256) {
+        const int c = idx / D, e = idx % D;
+        float top = PAGED_NO_MAX, l = 0.f, o = 0.f;
+        constexpr int AHEAD = 8;
+        for (int i0 = 0; i0 < n; i0 += AHEAD) {
+            float pm[AHEAD], pl[AHEAD], po[AHEAD];
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {   // (past the end: the last piece, which does not count)
+                const float* p = piece(min(i0 + k, n - 1)) + c * PF;
+                pm[k] = p[0];
+                pl[k] = p[1];
+                po[k] = p[2 + e];
+            }
+            float up = top;
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) up = i0 + k < n ? fmaxf(up, pm[k]) : up;
+            const float f = __builtin_amdgcn_exp2f(top - up);
+            top = up;
+            l *= f;
+            o *= f;
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                if (i0 + k >= n) continue;
+                const float w = __builtin_amdgcn_exp2f(pm[k] - top);
+                l += pl[k] * w;
+                o += po[k] * w;
+            }
+        }
+        const int col = C * ct + c, i = paged_token(a, col);
+        const size_t oc = (size_t)(rq.first + i) * a.Hq + g * a.G + (col - i * a.G);
+        const bool none = l == 0.f;
+        ((__bf16*)a.out)[oc * D + e] = (__bf16)(none ? 0.f : o * (1.0f / l));
+        if (e == 0 && a.lse != nullptr) a.lse[oc] = none ? -INFINITY : (top + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+    }
+}
+
+template <int D, int NC, bool ALIGNED>
+hipError_t launch(const PagedArgs& a, int max_ct, hipStream_t st) {
+    using Lds = StreamLds<D, NC>;
+    static_assert(sizeof(Lds) <= 80 * 1024, "two workgroups per compute unit");
+    // Raises the kernel's dynamic LDS limit, once per process.
+    static const hipError_t once = hipFuncSetAttribute(reinterpret_cast<const void*>(&paged_stream_kernel<D, NC, ALIGNED>),
+                                                       hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Lds));
+    if (once != hipSuccess) return once;
+    paged_stream_kernel<D, NC, ALIGNED><<<dim3((unsigned)(a.n_wg * a.Hkv)), dim3(64 * W), sizeof(Lds), st>>>(a);
+    if (a.n_wg > 1) paged_stream_join_kernel<D, NC><<<dim3((unsigned)(a.B * max_ct * a.Hkv)), dim3(256), 0, st>>>(a, max_ct);
+    return hipGetLastError();
+}
+
+template <int D, int NC>
+hipError_t launch(const PagedArgs& a, int max_ct, hipStream_t st) {
+    return a.P % StreamPiece<D, NC, true>::COPIES == 0 ? launch<D, NC, true>(a, max_ct, st) : launch<D, NC, false>(a, max_ct, st);
+}
+
+}  // namespace
+
+size_t paged_stream_partials_bytes(const Shape& s, int n_cu) {
+    return (size_t)std::max(2 * n_cu, s.Hkv) * 2 * 32 * (s.d + 2) * sizeof(float);
+}
+
+hipError_t launch_paged_stream(const Shape& s, const PagedArgs& args, int n_cu, hipStream_t st) {
+    PagedArgs a = args;
+    a.n_wg = std::max(1, 2 * n_cu / s.Hkv);   // two per compute unit are resident
+    const int64_t most = std::min<int64_t>((int64_t)a.max_new * s.G, a.cols_hi);
+    const int nc = most <= 16 ? 1 : 2;
+    const int max_ct = (int)((most + 16 * nc - 1) / (16 * nc));
+    if (s.d == 128) return nc == 1 ? launch<128, 1>(a, max_ct, st) : launch<128, 2>(a, max_ct, st);
+    return nc == 1 ? launch<64, 1>(a, max_ct, st) : launch<64, 2>(a, max_ct, st);
+}
+
+}  // namespace fr
