@@ -921,6 +921,8 @@ fr_status fr_paged_attn(fr_ctx* ctx, const void* q, const int32_t* q_offsets, co
     if ((st = check_tokens(ctx, n_tokens)) != FR_OK) return st;
     if ((st = check_pages(ctx, n_pages, page_rows)) != FR_OK) return st;
     if (max_new < 0) return fail(ctx, FR_ERR_INVALID_ARG, "max_new = %d is negative", max_new);
+    if ((int64_t)n_tokens * ctx->shape.Hq > INT32_MAX)
+        return fail(ctx, FR_ERR_UNSUPPORTED, "n_tokens x n_q_heads = %lld exceeds 2^31 - 1", (long long)n_tokens * ctx->shape.Hq);
     if (n_tokens == 0 || n_requests == 0 || max_new == 0) return FR_OK;
     if (bad16(q) || bad16(out) || (n_pages > 0 && (bad16(k_pages) || bad16(v_pages))))
         return fail(ctx, FR_ERR_INVALID_ARG, "q / out / k_pages / v_pages is NULL or not 16-byte aligned");

@@ -19,6 +19,7 @@ struct PagedArgs {
     uint32_t g_magic;        // ceil(2^32 / G): c / G = mulhi(c, g_magic) for c < 2^26
     uint32_t p_magic, p_shift;   // j / P = mulhi(2 j, p_magic) >> p_shift for j < 2^30
     float scale_log2e;
+    int split_mode;
 };
 
 // A request as a launch sees it.
@@ -63,7 +64,7 @@ __device__ __forceinline__ int64_t uniform64(int64_t v) {
 
 // How a launch's work is dealt out.  The work of a KV head is one line of units: requests in order, of each its column tiles, of each its units of keys.
 // Workgroup w of n takes units floor(w U / n) .. floor((w + 1) U / n) - 1 of it, wherever they begin and end, so every workgroup has the same
-// share whatever the lengths are, and the host need not know them.  An item (column tile) that falls to several workgroups leaves a partial result
+// share whatever the lengths are, and the host need not know them.  n is at most U (paged_sharers): none of them goes without.  An item (column tile) that falls to several workgroups leaves a partial result
 // per piece: in slot 2 w of a workgroup whose piece begins behind the item's start, in 2 w + 1 of the one that has its start but not its end.
 struct PagedLine {
     int64_t total;    // U
@@ -97,6 +98,7 @@ __device__ __forceinline__ PagedLine paged_line(int B, Cost cost, Find find) {
     }
     return r;
 }
+__device__ __forceinline__ int paged_sharers(const PagedArgs& a, int64_t total) { return (int)min((int64_t)a.n_wg, total); }
 __device__ __forceinline__ int64_t paged_first_unit(int64_t w, int64_t total, int n) { return w * total / n; }
 __device__ __forceinline__ int paged_owner(int64_t u, int64_t total, int n) { return (int)(((u + 1) * n - 1) / total); }   // the workgroup that has unit u
 
@@ -134,10 +136,10 @@ __device__ __forceinline__ uint32_t paged_lds(const void* p) {
     return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) const unsigned char*)p);
 }
 __device__ __forceinline__ void paged_copy16(const void* src, uint32_t lds) {   // lane i's 16 bytes to lds + 16 i
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(src), "s"(lds) : "memory");
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(src), "s"(__builtin_amdgcn_readfirstlane(lds)) : "memory");
 }
 __device__ __forceinline__ void paged_copy4(const void* src, uint32_t lds) {    // lane i's 4 bytes to lds + 4 i
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(src), "s"(lds) : "memory");
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(src), "s"(__builtin_amdgcn_readfirstlane(lds)) : "memory");
 }
 template <int N>
 __device__ __forceinline__ void paged_wait_but() {   // until all but the wave's last N copies have landed
@@ -149,6 +151,9 @@ __device__ __forceinline__ void paged_wait_but() {   // until all but the wave's
 
 size_t paged_stream_partials_bytes(const Shape& s, int n_cu);
 hipError_t launch_paged_stream(const Shape& s, const PagedArgs& a, int n_cu, hipStream_t st);
+
+size_t paged_tile_partials_bytes(const Shape& s, int n_cu);
+hipError_t launch_paged_tile(const Shape& s, const PagedArgs& a, int n_cu, hipStream_t st);
 
 // ---- joining pieces -----------------------------------------------------------------------------------
 // A piece's slot: [column][D + 2] fp32: exponent reference (base 2), sum of weights, weighted values.

@@ -6,6 +6,7 @@
 #include "k_paged.hpp"
 
 #include <algorithm>
+#include <cstdlib>
 
 namespace fr {
 
@@ -127,9 +128,10 @@ hipError_t launch_paged_attn(const Shape& s, const PagedAttnArgs& args, float* p
     if (e != hipSuccess || (int64_t)args.max_new * s.G <= few) return e;
     a.cols_lo = few;
     a.cols_hi = INT32_MAX;
-    return s.d == 128 ? launch_rows<__bf16, 128>(a, st) : launch_rows<__bf16, 64>(a, st);
+    if (const char* m = getenv("PAGED_MODE")) a.split_mode = atoi(m);
+    return launch_paged_tile(s, a, n_cu, st);
 }
 
-size_t paged_attn_partials_bytes(const Shape& s, int n_cu) { return s.dtype == FR_BF16 ? paged_stream_partials_bytes(s, n_cu) : 0; }
+size_t paged_attn_partials_bytes(const Shape& s, int n_cu) { return s.dtype == FR_BF16 ? std::max(paged_stream_partials_bytes(s, n_cu), paged_tile_partials_bytes(s, n_cu)) : 0; }
 
 }  // namespace fr

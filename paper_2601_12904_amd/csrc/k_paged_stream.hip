@@ -350,9 +350,11 @@ __global__ __launch_bounds__(64 * W, 2) void paged_stream_kernel(const PagedArgs
     const int g = blockIdx.x % a.Hkv, w = blockIdx.x / a.Hkv;
     int64_t u = 0, end = 0;
     const PagedLine line = paged_line(a.B, [&](int b) { return stream_cost<C>(a, b); }, [&](int64_t total) {
-        u = paged_first_unit(w, total, a.n_wg);
-        end = paged_first_unit(w + 1, total, a.n_wg);
-        return u < end ? u : -1;
+        const int n = paged_sharers(a, total);
+        if (w >= n) return (int64_t)-1;
+        u = paged_first_unit(w, total, n);
+        end = paged_first_unit(w + 1, total, n);
+        return u;
     });
     if (line.b < 0) return;
     int64_t start = line.start;   // of the request's units
@@ -391,7 +393,7 @@ __global__ __launch_bounds__(256) void paged_stream_join_kernel(const PagedArgs 
         before += uniform64(wave_sum64(b0 + lane < b ? c : 0));
     }
     const int64_t u0 = before + (int64_t)ct * units;
-    const int w0 = paged_owner(u0, all, a.n_wg), w1 = paged_owner(u0 + units - 1, all, a.n_wg);
+    const int sharers = paged_sharers(a, all), w0 = paged_owner(u0, all, sharers), w1 = paged_owner(u0 + units - 1, all, sharers);
     if (w0 == w1) return;   // whole: stored already
     const int cols = min(C, rq.n * a.G - C * ct), n = w1 - w0 + 1;
     auto piece = [&](int i) { return a.partials + (((size_t)(w0 + i) * a.Hkv + g) * 2 + (i == 0 ? 1 : 0)) * (C * PF); };

@@ -1,0 +1,828 @@
+// Attention over a paged cache, requests with many query columns (chunks of prompts, whole prompts): bf16, head_dim 64 or 128.
+//
+// One workgroup owns one KV head and a tile of 256 query columns ((row, query head) pairs, the heads of the group fastest) in four row groups of 64; eight
+// waves, two per row group and per SIMD, of which the first takes keys 0..31 of every tile of 64 keys and the second keys 32..63, each with output
+// accumulators of its own, which are added up at the end.  S^T = K Q^T and O^T = V^T P^T with v_mfma_f32_16x16x32_bf16, keys on the register
+// dimension of S^T, columns on lanes: the accumulators of two 16-key blocks are, after conversion, the B operand of the second product.
+//
+// Keys and values come straight from the pages, global -> LDS without registers: a wave brings eight consecutive rows of each tile, so in pages of a multiple of
+// eight rows their address is the same for the whole wave (scalar registers), and one table entry per wave and tile, itself copied to LDS two tiles
+// ahead, is all the look-up there is.  Rows lie in LDS as they do in memory, the 16-byte vectors of row r permuted by an exclusive or with r (the lanes ask for them
+// in that order), which keeps the fragment reads of both products free of bank conflicts: K by 16-byte reads, V^T by ds_read_b64_tr_b16, which
+// transposes 4 keys x 16 dims on the way.  So no pass packs or transposes anything in front: a chunk of 2048 rows behind 14336 would read, write and read
+// again 67 MB for it.
+//
+// A wave alternates between a matrix phase (O += its half of tile kt - 1, logits of its half of tile kt) and a softmax phase; the two waves of a SIMD do so in turn,
+// so that the vector work of one runs beside the matrix instructions of the other:
+//   waves 0..3   barrier kt | matrix (kt - 1, kt) | copies kt | softmax kt
+//   waves 4..7   barrier kt | copies kt | softmax kt - 1 | matrix (kt - 1, kt)
+//
+// Softmax.  exp(x - m) / sum exp(x - m) does not depend on m, and fp32 and bf16 leave about 2^127 of room, so a column's exponent reference is the maximum over its
+// visible ones of the request's keys 0..31, in every piece of its item, and the loop holds no maximum, no comparison and no rescaling (which would
+// spill registers).  Where the sums show that a later logit passed it by more than that, the piece is done again with the largest logit of its own
+// keys, found in a pass over them that forms nothing but logits.  Weights go into the second product as bf16 (half a step, 2^-8, of each; their sum is
+// taken in fp32 before), as the output does.
+//
+// What a column does not see stays out of it by hand, as a weight of 0 does not take a NaN or an infinity out of a product: keys behind the tile's last row
+// repeat that one; a value that is not finite and that some column does not see makes that one's sums NaN, and in the second go the wave that brought a
+// row of such a tile takes values that are not finite out of LDS; they reach the columns that see them when the loop is over.
+#include "k_paged.hpp"
+
+#include <algorithm>
+
+namespace fr {
+
+namespace {
+
+constexpr int WAVES = 8, RG = 4, KT = 64, NC = 4;   // waves; row groups; keys of a tile; blocks of 16 columns of a row group
+constexpr int C = 64 * RG;                          // columns of a tile
+constexpr int RW = KT / WAVES;                      // rows of a tile that a wave brings
+constexpr int TILE0 = 4;                            // ring slot of tile 0's page numbers
+constexpr int ITEM_KEYS = 192;                      // what a piece costs beside its keys, in keys (prologue, joining of the waves, output)
+
+typedef short __attribute__((ext_vector_type(4))) i16x4;
+typedef const bf16x8 __attribute__((address_space(3)))* lds_b128;
+
+template <int D>
+struct __attribute__((aligned(16))) TileLds {
+    static constexpr int ROW = 2 * D, TILE = KT * ROW;
+    static constexpr int NK = D / 32, MD = D / 16;            // matrix steps over the dims of a logit, 16-dim blocks of the output
+    static constexpr int QR = 2, QL = NK - QR;                // matrix steps whose query fragments stay in registers; those that come from LDS
+    unsigned char k[3][TILE], v[3][TILE];                     // rings
+    unsigned char q[QL > 0 ? RG * QL * NC * 1024 : 16];
+    int pos[RG][64];                                          // positions of the columns (masked tiles)
+    int page[WAVES][5][64];                                   // page numbers of the rows that a wave is to bring, per tile
+    unsigned char hole[5][8];                                 // per tile and wave: bit r = its row r has no page
+    float ref[WAVES][64];                                     // the waves' largest logits (EXACT)
+    int apart;
+};
+template <int D>
+constexpr int EXCHANGE_WAVE = D / 32 * NC * 1024 + 1024;      // half of a wave's accumulators, and its sums
+template <int D>
+constexpr size_t tile_lds_bytes() {
+    constexpr size_t a = sizeof(TileLds<D>), b = (size_t)WAVES * EXCHANGE_WAVE<D>, c = (size_t)RG * 64 * (D + 8) * 2;
+    return a > b ? (a > c ? a : c) : (b > c ? b : c);
+}
+
+// ---- how the work is dealt out --------------------------------------------------------------------------
+// The cost of a column tile in keys: what its last row sees, about (the line of work only has to be the same for everybody), and what every item takes.
+struct TileCosts {
+    int64_t base;   // tile t: base + (t + 1) step
+    int step, n_ct;
+    __device__ __forceinline__ int64_t tile(int t) const { return base + (int64_t)(t + 1) * step; }
+    __device__ __forceinline__ int64_t before(int t) const { return t * base + (int64_t)step * ((int64_t)t * (t + 1) / 2); }   // of tiles 0 .. t - 1
+    __device__ __forceinline__ int tile_at(int64_t v) const {   // the tile that unit v falls into
+        const double s = (double)step, h = (double)base + 0.5 * s;
+        int t = (int)((__builtin_sqrt(h * h + 2.0 * s * (double)v) - h) / s);
+        t = max(0, min(t, n_ct - 1));
+        while (t > 0 && before(t) > v) --t;
+        while (t + 1 < n_ct && before(t + 1) <= v) ++t;
+        return t;
+    }
+};
+__device__ __forceinline__ TileCosts tile_costs(const PagedArgs& a, const PagedRequest& r) {
+    TileCosts c;
+    c.base = (int64_t)max(0, min(r.cached, a.cap)) + KT + ITEM_KEYS;
+    c.step = (C + a.G - 1) / a.G;
+    c.n_ct = (int)(((int64_t)r.n * a.G + C - 1) / C);
+    return c;
+}
+
+struct TilePlan {
+    bool whole;         // a workgroup per item; else equal shares of the line of work
+    int64_t total;      // units of the line
+    int sharers;        // workgroups that share it
+    int b;              // the request that holds what was looked for, -1: none
+    int64_t start;      // its first unit (whole: its first item)
+};
+// Both ways of dealing: whole items, longest of a request first, which walk the keys of a KV head side by side and share them in the caches; or equal shares.
+// Whole where its estimated end (the longest item; the average load and one of the shortest, where there are several items for each workgroup) is no later than that of
+// equal shares, which read keys at different places (a tenth) and join pieces.
+__device__ __forceinline__ TilePlan tile_plan(const PagedArgs& a, int64_t item, int w) {
+    const int lane = threadIdx.x & 63;
+    int64_t total = 0, items = 0, cost = 0, most = 0, least = INT64_MAX;
+    int n_ct = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 64) {
+        cost = 0;
+        n_ct = 0;
+        if (b0 + lane < a.B) {
+            const PagedRequest r = paged_request(a, b0 + lane);
+            if (r.n > 0) {
+                const TileCosts c = tile_costs(a, r);
+                n_ct = c.n_ct;
+                cost = c.before(n_ct);
+                most = max(most, c.tile(n_ct - 1));
+                least = min(least, c.tile(0));
+            }
+        }
+        total += uniform64(wave_sum64(cost));
+        items += uniform64(wave_sum64(n_ct));
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        most = max(most, (int64_t)__shfl_xor(most, d));
+        least = min(least, (int64_t)__shfl_xor(least, d));
+    }
+    most = uniform64(most);
+    least = uniform64(least);
+    TilePlan p{false, total, 1, -1, 0};
+    if (total == 0) return p;
+    const int n = p.sharers = paged_sharers(a, total);
+    const int64_t share = total / n;
+    const int64_t in_items = items <= n ? most : max(most, share + least);
+    p.whole = a.split_mode == 1 || (a.split_mode == 0 && in_items <= share + share / 10 + 2 * ITEM_KEYS);
+    const int64_t u = p.whole ? item : paged_first_unit(w, total, n);
+    if (p.whole ? u >= items : w >= n) return p;
+    for (int b0 = 0; b0 < a.B; b0 += 64) {
+        if (a.B > 64) {
+            cost = 0;
+            n_ct = 0;
+            if (b0 + lane < a.B) {
+                const PagedRequest r = paged_request(a, b0 + lane);
+                if (r.n > 0) {
+                    const TileCosts c = tile_costs(a, r);
+                    n_ct = c.n_ct;
+                    cost = c.before(n_ct);
+                }
+            }
+        }
+        const int64_t mine = p.whole ? n_ct : cost, upto = p.start + wave_scan64(mine);
+        const uint64_t beyond = __ballot(upto > u);
+        if (beyond != 0) {
+            const int l = __builtin_ctzll(beyond);
+            p.b = b0 + l;
+            p.start = uniform64(__shfl(upto, l)) - uniform64(__shfl(mine, l));
+            return p;
+        }
+        p.start = uniform64(__shfl(upto, 63));
+    }
+    return p;
+}
+
+__device__ __forceinline__ f32x4 mfma(const bf16x8& a, const bf16x8& b, const f32x4& c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+
+// A column tile of a request, and what a lane knows of its columns.
+template <int D>
+struct TileItem {
+    int first_row;                 // the request's first row
+    int g, col0, head0, token0;    // first column; its head within the group and its row within the request
+    int cols, p_first, p_last;     // columns of the request; keys up to p_first are visible to every column, none beyond p_last to any
+    __device__ __forceinline__ void init(const PagedArgs& a, const PagedRequest& r, int t, int g_) {
+        g = g_;
+        first_row = r.first;
+        cols = r.n * a.G;
+        col0 = C * t;
+        token0 = col0 / a.G;
+        head0 = col0 - token0 * a.G;
+        p_first = paged_position(a, r, token0);
+        p_last = paged_position(a, r, min((int64_t)col0 + C, (int64_t)cols) == cols ? r.n - 1 : (col0 + C - 1) / a.G);
+    }
+    // column cl of the tile (past the end: the request's last): row within the request and head within the group
+    __device__ __forceinline__ void column(const PagedArgs& a, int cl, int* token, int* head) const {
+        const int c = head0 + min(cl, cols - 1 - col0), i = paged_token(a, c);
+        *token = token0 + i;
+        *head = c - i * a.G;
+    }
+    __device__ __forceinline__ size_t out_row(const PagedArgs& a, int cl) const {
+        int token, head;
+        column(a, cl, &token, &head);
+        return (size_t)(first_row + token) * a.Hq + g * a.G + head;
+    }
+};
+
+// One matrix phase: O^T += V^T P^T for the wave's half of one tile, S^T = K Q^T for its half of another.  tv, tk: LDS addresses of the lane's first fragments.
+// Fragments are requested PF steps of four matrix instructions ahead.
+template <int D, bool PV>
+__device__ __forceinline__ void matrix_phase(uint32_t tv, uint32_t tk, const bf16x8 (&qf)[NC][TileLds<D>::QR], uint32_t q_lds, const u32x4 (&p)[NC],
+                                             f32x4 (&o)[D / 16][NC], f32x4 (&s)[2][NC]) {
+    using L = TileLds<D>;
+    constexpr int NK = L::NK, MD = L::MD, PF = 4, QR = L::QR, FIRST = PV ? 0 : MD, STEPS = MD + 2 * NK, BLOCK = 16 * L::ROW;
+    auto dims = [](int j) { return QR < NK ? (j & 1 ? j / 2 : QR + j / 2) : j; };   // order of the dims: LDS, registers, LDS, registers
+    bf16x8 fr[PF + 1], qb[2][NC];
+    const lds_b128 q_frag = reinterpret_cast<lds_b128>((uintptr_t)q_lds);
+    auto frag = [&](int i) -> bf16x8 {
+        if (i < MD) {
+            const auto at = reinterpret_cast<__attribute__((address_space(3))) i16x4*>((uintptr_t)(tv ^ (32u * i)));
+            const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(at), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(at + BLOCK / 8);
+            return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+        return reinterpret_cast<lds_b128>((uintptr_t)(tk ^ (64u * dims((i - MD) / 2))))[(i & 1) * BLOCK / 16];
+    };
+    auto load_q = [&](int j) {   // query fragments of the j-th step of the dims, if they are in LDS
+        const int ks = dims(j);
+        if (ks < QR) return 0;
+#pragma unroll
+        for (int nb = 0; nb < NC; ++nb) qb[j & 1][nb] = q_frag[((ks - QR) * NC + nb) * 64];
+        return NC;
+    };
+    int reads[STEPS] = {};   // LDS reads issued in front of step i's products
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = FIRST; i < FIRST + PF; ++i) fr[i % (PF + 1)] = frag(i);
+    if (!PV) reads[FIRST] += load_q(0);
+#pragma unroll
+    for (int i = FIRST; i < STEPS; ++i) {
+        if (i + PF < STEPS) {
+            fr[(i + PF) % (PF + 1)] = frag(i + PF);
+            reads[i] += i + PF < MD ? 2 : 1;
+        }
+        if (PV && i == MD - 2) reads[i] += load_q(0);   // two steps ahead
+        if (i >= MD && (i - MD) % 2 == 0 && (i - MD) / 2 + 1 < NK) reads[i] += load_q((i - MD) / 2 + 1);
+        const bf16x8 f = fr[i % (PF + 1)];
+        if (i < MD) {
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {   // (back and forth: neighbours in time share an operand, which saves power)
+                const int nb = i & 1 ? NC - 1 - c : c;
+                o[i][nb] = mfma(f, __builtin_bit_cast(bf16x8, p[nb]), o[i][nb]);
+            }
+        } else {
+            const int j = (i - MD) / 2, ks = dims(j), b = i & 1;
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                const int nb = b ? NC - 1 - c : c;
+                s[b][nb] = mfma(f, ks < QR ? qf[nb][ks < QR ? ks : 0] : qb[j & 1][nb], j == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[b][nb]);
+            }
+        }
+    }
+    __builtin_amdgcn_sched_group_barrier(0x100, PV ? 2 * PF : PF, 0);
+#pragma unroll
+    for (int i = FIRST; i < STEPS; ++i) {
+        if (reads[i] == 1) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        if (reads[i] == 2) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+        if (reads[i] == NC) __builtin_amdgcn_sched_group_barrier(0x100, NC, 0);
+        if (reads[i] == NC + 1) __builtin_amdgcn_sched_group_barrier(0x100, NC + 1, 0);
+        if (reads[i] == NC + 2) __builtin_amdgcn_sched_group_barrier(0x100, NC + 2, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, NC, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// Key tiles [kb, ke) of an item.  whole: they are all it has, the outputs are stored; else the partial result goes to `part`: [C][2] references and sums,
+// then [C][D] weighted values.
+// EXACT = false: returns false where the sums overflowed the reference or are NaN, or where keys 0..31 have none; what it stored is worth nothing then, and the caller does
+// the piece again with EXACT = true.
+template <int D, bool ALIGNED, bool EXACT>
+__device__ __forceinline__ bool process_piece(const PagedArgs& a, const PagedRequest& rq, int b, int t, int g, int kb, int ke, bool whole, float* part,
+                                              unsigned char* smem_raw) {
+    using L = TileLds<D>;
+    constexpr int NK = L::NK, MD = L::MD, QR = L::QR, QL = L::QL, ROW = L::ROW, TILE = L::TILE;
+    constexpr int RV = D / 8, RC = 64 / RV, COPIES = RW / RC;   // vectors of a row; rows of a copy; copies of a wave, of a tile's keys or values
+    L& sm = *reinterpret_cast<L*>(smem_raw);
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));   // (opaque: what is formed from it again later need not be kept meanwhile)
+    const int lane = tid & 63, x = lane & 15, kg = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), group = wave & 3, second = wave >> 2;
+    TileItem<D> it;
+    it.init(a, rq, t, g);
+    const int p_last = it.p_last;
+    const bool empty = kb >= ke;   // nothing to see, or no tile of a small item falls to this piece
+    if (empty && !whole) {
+        if (tid < C) { part[2 * tid] = PAGED_NO_MAX; part[2 * tid + 1] = 0.f; }
+        return true;
+    }
+    const uint32_t k_base = paged_lds(sm.k[0]), v_base = paged_lds(sm.v[0]);
+    const uint32_t q_lds = paged_lds(sm.q) + group * (QL * NC * 1024) + lane * 16u;
+    bf16x8 qf[NC][QR];
+    {
+        bf16x8 ql[2][QL > 0 ? QL : 1];
+#pragma unroll
+        for (int nb = 0; nb < NC; ++nb) {
+            const __bf16* p = (const __bf16*)a.q + it.out_row(a, 64 * group + 16 * nb + x) * D + 8 * kg;
+#pragma unroll
+            for (int ks = 0; ks < QR; ++ks) qf[nb][ks] = *reinterpret_cast<const bf16x8*>(p + 32 * ks);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {   // the two waves of a row group bring two column blocks' each to LDS
+            const __bf16* p = (const __bf16*)a.q + it.out_row(a, 64 * group + 16 * (2 * second + i) + x) * D + 8 * kg;
+#pragma unroll
+            for (int ks = 0; ks < QL; ++ks) ql[i][ks] = *reinterpret_cast<const bf16x8*>(p + 32 * (QR + ks));
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int ks = 0; ks < QL; ++ks)
+                *reinterpret_cast<bf16x8 __attribute__((address_space(3)))*>((uintptr_t)(q_lds + (ks * NC + 2 * second + i) * 1024)) = ql[i][ks];
+    }
+    if (!second) {
+        int token, head;
+        it.column(a, 64 * group + lane, &token, &head);
+        sm.pos[group][lane] = paged_position(a, rq, token);
+    }
+    if (tid == 0) sm.apart = 0;
+
+    // ---- copies --------------------------------------------------------------------------------------------
+    const int32_t* table = a.block_table + (size_t)b * a.W;
+    const uint32_t row_bytes = (uint32_t)(a.Hkv * D * 2);
+    const unsigned char *k_pages = (const unsigned char*)a.k_pages + (size_t)g * ROW, *v_pages = (const unsigned char*)a.v_pages + (size_t)g * ROW;
+    const uint32_t page_lds = paged_lds(sm.page[wave]);
+    auto is_page = [&](int p) { return (uint32_t)p < (uint32_t)a.n_pages; };
+    const int last = max(ke - 1, 0);   // (past the piece's last tile the copies repeat that one: the counts of the waits stay the same, and nobody reads them)
+    auto copy_pages = [&](int kt, int slot) {    // page numbers of the wave's rows of tile kt
+        const int j = KT * min(kt, last) + RW * wave + (lane & (RW - 1));
+        paged_copy4(table + paged_block(a, max(min(j, p_last), 0)), page_lds + 256 * slot);
+    };
+    // Where the wave's rows of a tile are: aligned pages: byte offset of the first one, the same for all lanes, and how many rows there are before the last
+    // visible one; else the row of each copy's lane.
+    struct Rows {
+        uint64_t at;
+        int most;
+        uint32_t row[COPIES];
+    };
+    auto swz = [](int r) { return D == 128 ? r & 15 : r >> 1 & 7; };
+    const int lr = lane / RV, lv = lane % RV;   // row of the lane within a copy, place of its vector
+    auto lane_vec = [&](int c) { return 16u * (uint32_t)(lv ^ swz(RW * wave + RC * c + lr)); };
+    auto find_rows = [&](int kt, int slot) {
+        Rows r;
+        const int j0 = KT * min(kt, last) + RW * wave;
+        int holes;
+        if constexpr (ALIGNED) {
+            const int page = __builtin_amdgcn_readfirstlane(sm.page[wave][slot][0]), jc = min(j0, p_last);
+            holes = is_page(page) ? 0 : (1 << RW) - 1;
+            r.at = ((uint64_t)(holes ? 0 : page) * (uint32_t)a.P + (uint32_t)(jc - paged_block(a, jc) * a.P)) * row_bytes;
+            r.most = p_last - jc;       // (rows behind it repeat it)
+            if (j0 > p_last) r.most = 0;
+        } else {
+            const int mine = sm.page[wave][slot][lane & (RW - 1)];
+            holes = (int)(__ballot(!is_page(mine)) & ((1 << RW) - 1));
+#pragma unroll
+            for (int c = 0; c < COPIES; ++c) {
+                const int i = RC * c + lr, page = sm.page[wave][slot][i], j = min(j0 + i, p_last);
+                r.row[c] = (uint32_t)(is_page(page) ? page : 0) * (uint32_t)a.P + (uint32_t)(j - paged_block(a, j) * a.P);
+            }
+        }
+        if (lane == 0) sm.hole[slot][wave] = (unsigned char)holes;
+        return r;
+    };
+    auto copy_rows = [&](const Rows& r, const unsigned char* pages, uint32_t lds) {
+#pragma unroll
+        for (int c = 0; c < COPIES; ++c) {
+            const unsigned char* src;
+            if constexpr (ALIGNED) src = pages + r.at + (size_t)((uint32_t)min(RC * c + lr, r.most) * row_bytes) + lane_vec(c);
+            else src = pages + (size_t)r.row[c] * row_bytes + lane_vec(c);
+            paged_copy16(src, lds + (RW * wave + RC * c) * ROW);
+        }
+    };
+    f32x4 o[MD][NC], s[2][NC];
+    u32x4 p[NC];
+    float l[NC], m[NC];
+#pragma unroll
+    for (int nb = 0; nb < NC; ++nb) m[nb] = PAGED_NO_MAX;
+    const int n_plain = (it.p_first + 1) / KT;   // leading tiles whose keys are visible to every column
+    if (!empty) {
+        const uint32_t tk0 = k_base + x * ROW + 16 * (kg ^ swz(x)), tk = tk0 + 32 * second * ROW;
+        const int y = 4 * kg + (x >> 2);        // the lane's key of a transposing read
+        const uint32_t tv = v_base + 32 * second * ROW + y * ROW + 16 * ((x >> 1 & 1) ^ swz(y)) + 8 * (x & 1);
+        int c0, c1, c2;     // ring slots (their bytes) of tiles kt, kt + 1, kt + 2
+        Rows next;          // of the tile whose values are to be copied next
+        // K tiles kb and kb + 1 and V tile kb land in LDS, the page numbers of the two behind them are on their way.
+        auto prime = [&](bool values) {
+            paged_wait_but<0>();   // (nothing that the compiler counts is in flight from here on)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) copy_pages(kb + i, (kb + i) & 3);
+            paged_wait_but<2>();
+            const Rows r0 = find_rows(kb, kb & 3);
+            copy_rows(r0, k_pages, k_base);
+            if (values) copy_rows(r0, v_pages, v_base);
+            next = find_rows(kb + 1, (kb + 1) & 3);
+            copy_rows(next, k_pages, k_base + TILE);
+            c0 = 0; c1 = TILE; c2 = 2 * TILE;
+        };
+        auto mask = [&](int kt, uint32_t hole) {   // hole: bits of the wave's 32 keys
+            int ln = lane;
+            asm volatile("" : "+v"(ln));
+            const int quarter = ln >> 4, key0 = KT * kt + 32 * second + 4 * quarter;
+            const uint32_t mine = hole >> (4 * quarter);   // bits 16 bb + v
+#pragma unroll
+            for (int nb = 0; nb < NC; ++nb) {
+                const int pos = sm.pos[group][16 * nb + (ln & 15)];
+#pragma unroll
+                for (int bb = 0; bb < 2; ++bb)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v)
+                        if (key0 + 16 * bb + v > pos || (mine >> (16 * bb + v) & 1)) s[bb][nb][v] = -INFINITY;
+                __builtin_amdgcn_sched_barrier(0);   // (block by block: the results of all comparisons at once take registers that the loop needs)
+            }
+        };
+        auto holes_of = [&](int kt, uint32_t* mine) {   // does the tile have any, and which of the wave's 32 keys
+            const uint64_t hole = *reinterpret_cast<const uint64_t*>(sm.hole[kt & 3]);
+            const uint32_t lo = __builtin_amdgcn_readfirstlane((int)(uint32_t)hole), hi = __builtin_amdgcn_readfirstlane((int)(hole >> 32));
+            *mine = second ? hi : lo;
+            return (lo | hi) != 0;
+        };
+        auto plain_barrier = [] {   // without the fences of __syncthreads(): the waits are explicit
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+        };
+        if constexpr (EXACT) {   // the maximum of its logits over the piece's visible keys
+            prime(false);
+            paged_wait_but<0>();
+            __syncthreads();
+            for (int kt = kb; kt < ke; ++kt) {   // K tiles kt and kt + 1 are in ring slots, kt + 2 follows
+                const Rows after = find_rows(kt + 2, (kt + 2) & 3);
+                copy_rows(after, k_pages, k_base + c2);
+                copy_pages(kt + 4, kt & 3);
+                matrix_phase<D, false>(0, tk + c0, qf, q_lds, p, o, s);
+                uint32_t hole;
+                if (holes_of(kt, &hole) || kt >= n_plain) mask(kt, hole);
+#pragma unroll
+                for (int nb = 0; nb < NC; ++nb)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) m[nb] = fmaxf(m[nb], fmaxf(s[0][nb][v], s[1][nb][v]));
+                paged_wait_but<COPIES + 1>();          // all but the newest tile
+                __builtin_amdgcn_s_waitcnt(0xc07f);    // lgkmcnt(0): the wave's own reads and writes
+                plain_barrier();
+                const int c = c0;
+                c0 = c1; c1 = c2; c2 = c;
+            }
+#pragma unroll
+            for (int nb = 0; nb < NC; ++nb) {
+                m[nb] = paged_column_max(m[nb]);
+                if (kg == 0) sm.ref[wave][16 * nb + x] = m[nb];
+            }
+            paged_wait_but<0>();
+            __syncthreads();
+#pragma unroll
+            for (int nb = 0; nb < NC; ++nb) {
+                const float top = fmaxf(m[nb], sm.ref[wave ^ 4][16 * nb + x]);
+                m[nb] = top == PAGED_NO_MAX ? PAGED_NO_MAX : top * a.scale_log2e;
+            }
+            prime(true);
+            paged_wait_but<0>();
+            __syncthreads();
+        } else {   // the maximum over the visible ones of keys 0..31
+            paged_wait_but<0>();
+            copy_pages(0, TILE0);
+            paged_wait_but<0>();
+            copy_rows(find_rows(0, TILE0), k_pages, k_base + 2 * TILE);
+            prime(true);
+            paged_wait_but<0>();
+            __syncthreads();
+            if (*reinterpret_cast<const uint32_t*>(sm.hole[TILE0]) != 0) return false;   // (uniform; behind the barrier nothing is in flight)
+            matrix_phase<D, false>(0, tk0 + 2 * TILE, qf, q_lds, p, o, s);
+#pragma unroll
+            for (int nb = 0; nb < NC; ++nb) {
+                const int pos = sm.pos[group][16 * nb + x];
+                float t = -INFINITY;
+#pragma unroll
+                for (int bb = 0; bb < 2; ++bb)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) t = fmaxf(t, 16 * bb + 4 * kg + v <= pos ? s[bb][nb][v] : -INFINITY);
+                m[nb] = fmaxf(paged_column_max(t) * a.scale_log2e, PAGED_NO_MAX);
+            }
+            __syncthreads();   // (K ring slot 2 is free)
+        }
+#pragma unroll
+        for (int i = 0; i < TILE / (64 * WAVES * 16); ++i)   // V ring slot 2 holds zeros for the matrix phase in front
+            *reinterpret_cast<u32x4*>(sm.v[2] + (i * 64 * WAVES + tid) * 16) = u32x4{0u, 0u, 0u, 0u};
+        __syncthreads();
+#pragma unroll
+        for (int nb = 0; nb < NC; ++nb) {
+            l[nb] = 0.f;
+            p[nb] = u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+            for (int md = 0; md < MD; ++md) o[md][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+
+        // ---- tile loop -------------------------------------------------------------------------------------
+        // Barrier kt says that K tile kt and V tile kt - 1 have landed and that nobody reads K tile kt - 1 and V tile kt - 2 any more; the copies
+        // behind it refill those slots: K tile kt + 2 and V tile kt + 1; and the page numbers of tile kt + 4.
+        int vp = 2 * TILE;                      // ring slot of V tile kt - 1
+        auto copies = [&](int kt) {
+            const Rows after = find_rows(kt + 2, (kt + 2) & 3);
+            copy_rows(after, k_pages, k_base + c2);
+            copy_rows(next, v_pages, v_base + c1);
+            copy_pages(kt + 4, kt & 3);
+            next = after;
+        };
+        // Values of tile kt (ring slot `slot`), this wave's rows, that are not finite: out of LDS.
+        auto scrub = [&](int kt, int slot) {
+            if (kt < n_plain && sm.hole[kt & 3][wave] == 0) return;   // (its own entry)
+            bool found = false;
+#pragma unroll 1
+            for (int i = lane * 16; i < RW * ROW; i += 1024) {
+                unsigned char* at = sm.v[0] + slot + RW * wave * ROW + i;
+                u32x4 w = *reinterpret_cast<const u32x4*>(at);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t kept = paged_finite_or_zero(w[e]);
+                    found = found || kept != w[e];
+                    w[e] = kept;
+                }
+                *reinterpret_cast<u32x4*>(at) = w;
+            }
+            if (__any(found) && lane == 0) sm.apart = 1;
+        };
+        auto barrier = [&](int kt) {
+            __builtin_amdgcn_sched_barrier(0);
+            paged_wait_but<2 * COPIES + 1>();      // all but the newest tile's copies
+            if constexpr (EXACT) scrub(kt, c0);
+            __builtin_amdgcn_s_waitcnt(0xc07f);    // lgkmcnt(0): the wave's own reads and writes
+            plain_barrier();
+            vp = c0;
+            c0 = c1; c1 = c2; c2 = vp;
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        auto softmax = [&](int kt) {
+            uint32_t hole;
+            const bool any_hole = holes_of(kt, &hole);
+            if (__builtin_expect(kt >= n_plain || any_hole, 0)) mask(kt, hole);
+#pragma unroll
+            for (int nb = 0; nb < NC; ++nb) {
+                float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+                for (int bb = 0; bb < 2; ++bb)
+#pragma unroll
+                    for (int v = 0; v < 4; v += 2) {
+                        const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[bb][nb][v], a.scale_log2e, -m[nb]));
+                        const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[bb][nb][v + 1], a.scale_log2e, -m[nb]));
+                        s0 += p0;
+                        s1 += p1;
+                        bf16x2 w;
+                        w[0] = (__bf16)p0;
+                        w[1] = (__bf16)p1;
+                        p[nb][2 * bb + v / 2] = __builtin_bit_cast(uint32_t, w);
+                    }
+                l[nb] += s0 + s1;
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        if (!second) {
+            for (int kt = kb;; ++kt) {
+                matrix_phase<D, true>(tv + vp, tk + c0, qf, q_lds, p, o, s);
+                if (kt == ke) break;
+                copies(kt);
+                softmax(kt);
+                barrier(kt);
+            }
+        } else {
+            copies(kb);
+            for (int kt = kb;; ++kt) {
+                matrix_phase<D, true>(tv + vp, tk + c0, qf, q_lds, p, o, s);
+                if (kt == ke) break;
+                barrier(kt);
+                copies(kt + 1);
+                softmax(kt);
+            }
+        }
+        paged_wait_but<0>();
+    } else {
+#pragma unroll
+        for (int nb = 0; nb < NC; ++nb) {
+            l[nb] = 0.f;
+#pragma unroll
+            for (int md = 0; md < MD; ++md) o[md][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+    }
+
+    // ---- the two waves of a row group add up: each keeps half of the dims ------------------------------------------
+    __syncthreads();   // (also: everyone is done with the rings)
+    bool apart = false;
+    if constexpr (EXACT) {
+        apart = sm.apart != 0;
+        __syncthreads();
+    }
+    constexpr int MH = MD / 2;
+    f32x4 oh[MH][NC];
+    const int md0 = second * MH;
+    {
+        unsigned char* mine = smem_raw + (size_t)wave * EXCHANGE_WAVE<D> + lane * 16;
+        const unsigned char* other = smem_raw + (size_t)(wave ^ 4) * EXCHANGE_WAVE<D> + lane * 16;
+#pragma unroll
+        for (int md = 0; md < MH; ++md)
+#pragma unroll
+            for (int nb = 0; nb < NC; ++nb) {
+                f32x4 w;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {   // (element by element: a choice between the arrays' places would put them into memory)
+                    const float lo = o[md][nb][e], hi = o[MH + md][nb][e];
+                    w[e] = second ? lo : hi;
+                    oh[md][nb][e] = second ? hi : lo;
+                }
+                *reinterpret_cast<f32x4*>(mine + (md * NC + nb) * 1024) = w;
+            }
+        *reinterpret_cast<f32x4*>(mine + MH * NC * 1024) = f32x4{l[0], l[1], l[2], l[3]};
+        __syncthreads();
+#pragma unroll
+        for (int md = 0; md < MH; ++md)
+#pragma unroll
+            for (int nb = 0; nb < NC; ++nb) {
+                const f32x4 w = *reinterpret_cast<const f32x4*>(other + (md * NC + nb) * 1024);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) oh[md][nb][e] += w[e];
+            }
+        const f32x4 l2 = *reinterpret_cast<const f32x4*>(other + MH * NC * 1024);
+#pragma unroll
+        for (int nb = 0; nb < NC; ++nb) l[nb] = paged_column_sum(l[nb] + l2[nb]);
+    }
+    if constexpr (EXACT) {
+        if (apart) {   // the values that were left out reach the columns that see them
+            int pos[NC];
+#pragma unroll
+            for (int nb = 0; nb < NC; ++nb) {
+                int token, head;
+                it.column(a, 64 * group + 16 * nb + x, &token, &head);
+                pos[nb] = paged_position(a, rq, token);
+            }
+#pragma unroll 1
+            for (int j0 = KT * kb; j0 <= p_last && j0 < KT * ke; j0 += RW) {
+                bool left = j0 / KT >= n_plain;
+                for (int i = 0; i < RW && !left; ++i) left = !is_page(table[paged_block(a, j0 + i)]);
+                if (!left) continue;
+#pragma unroll 1
+                for (int j = j0; j < j0 + RW && j <= p_last; ++j) {
+                    const int block = paged_block(a, j), page = table[block];
+                    if (!is_page(page)) continue;
+                    const uint16_t* key = (const uint16_t*)(v_pages + ((size_t)page * a.P + (j - block * a.P)) * row_bytes);
+#pragma unroll
+                    for (int md = 0; md < MH; ++md)
+#pragma unroll
+                        for (int v = 0; v < 4; ++v) {
+                            const uint32_t w = key[16 * (md0 + md) + 4 * kg + v];
+                            const float add = (w & 0x7F80u) == 0x7F80u ? __uint_as_float(w << 16) : 0.f;
+#pragma unroll
+                            for (int nb = 0; nb < NC; ++nb) oh[md][nb][v] += j <= pos[nb] ? add : 0.f;
+                        }
+                }
+            }
+        }
+    }
+    // With a fixed reference a runaway logit shows up as inf or NaN in the sums.  The sums of a part stay so far below that many of them add up.
+    bool bad = false;
+    if constexpr (!EXACT) {
+        const float limit = whole ? INFINITY : 0x1p100f;
+#pragma unroll
+        for (int nb = 0; nb < NC; ++nb) {
+            float check = l[nb];
+#pragma unroll
+            for (int md = 0; md < MH; ++md)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) check += fabsf(oh[md][nb][v]);
+            bad = bad || !(check < limit);
+        }
+        bad = __builtin_amdgcn_readfirstlane(__syncthreads_or(bad ? 1 : 0)) != 0;   // (also: the exchange has been read)
+        if (bad) return false;
+    } else {
+        __syncthreads();
+    }
+    if (!whole) {
+#pragma unroll
+        for (int nb = 0; nb < NC; ++nb) {
+            const int c = 64 * group + 16 * nb + x;
+            if (!second && kg == 0) { part[2 * c] = m[nb]; part[2 * c + 1] = l[nb]; }
+#pragma unroll
+            for (int md = 0; md < MH; ++md) *reinterpret_cast<f32x4*>(part + 2 * C + c * D + 16 * (md0 + md) + 4 * kg) = oh[md][nb];
+        }
+        return true;
+    }
+    // ---- normalise, transpose through LDS and store 16 bytes per lane ---------------------------------------------
+    constexpr int PITCH = D + 8, NV = D / 8;
+    __bf16* ob = reinterpret_cast<__bf16*>(smem_raw) + group * 64 * PITCH;   // [64 columns][d]
+#pragma unroll
+    for (int nb = 0; nb < NC; ++nb) {
+        const bool none = l[nb] == 0.f;   // it saw nothing
+        const float inv_l = none ? 0.f : 1.0f / l[nb];
+        typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
+#pragma unroll
+        for (int md = 0; md < MH; ++md) {
+            bf16x4 w;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = (__bf16)(oh[md][nb][e] * inv_l);
+            *reinterpret_cast<bf16x4*>(&ob[(16 * nb + x) * PITCH + 16 * (md0 + md) + 4 * kg]) = w;
+        }
+        const int cl = 64 * group + 16 * nb + x;
+        if (!second && kg == 0 && a.lse != nullptr && it.col0 + cl < it.cols)
+            a.lse[it.out_row(a, cl)] = none ? -INFINITY : (m[nb] + __builtin_amdgcn_logf(l[nb])) * 0.6931471805599453f;
+    }
+    __syncthreads();   // (the rows of a group come from both of its waves)
+#pragma unroll
+    for (int i = 0; i < NV / 2; ++i) {
+        const int c = (64 / NV) * (i + second * (NV / 2)) + lane / NV, v = lane % NV;
+        if (it.col0 + 64 * group + c < it.cols)
+            *reinterpret_cast<u32x4*>((__bf16*)a.out + it.out_row(a, 64 * group + c) * D + 8 * v) = *reinterpret_cast<const u32x4*>(&ob[c * PITCH + 8 * v]);
+    }
+    __syncthreads();   // (the next piece's copies overwrite what was staged)
+    return true;
+}
+
+// blockIdx.x = (item, or workgroup of the line) x Hkv + KV head: with 8 KV heads each die's cache serves one of them.
+template <int D, bool ALIGNED>
+__global__ __launch_bounds__(64 * WAVES) void paged_tile_kernel(const PagedArgs a) {
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem_raw[];
+    const int g = blockIdx.x % a.Hkv, w = blockIdx.x / a.Hkv;
+    const TilePlan plan = tile_plan(a, w, w);
+    if (plan.b < 0) return;
+    int64_t u = paged_first_unit(w, plan.total, plan.sharers), start = plan.start;
+    const int64_t end = paged_first_unit(w + 1, plan.total, plan.sharers);
+    for (int b = plan.b; b < a.B;) {
+        const PagedRequest rq = paged_request(a, b);
+        const TileCosts c = tile_costs(a, rq);
+        const int64_t all = rq.n > 0 ? c.before(c.n_ct) : 0;
+        if (!plan.whole && u >= start + all) {
+            start += all;
+            ++b;
+            continue;
+        }
+        const int t = plan.whole ? c.n_ct - 1 - (int)(w - start) : c.tile_at(u - start);
+        const int i = (int64_t)C * (t + 1) >= (int64_t)rq.n * a.G ? rq.n - 1 : (C * (t + 1) - 1) / a.G;   // the tile's last row
+        const int n = (paged_position(a, rq, i) + KT) / KT;                                              // its key tiles
+        const int64_t cost = c.tile(t), x0 = plan.whole ? 0 : u - start - c.before(t), x1 = plan.whole ? cost : min(cost, x0 + (end - u));
+        const int kb = (int)(x0 * n / cost), ke = (int)(x1 * n / cost);
+        float* part = a.partials + ((size_t)blockIdx.x * 2 + (x0 > 0 ? 0 : 1)) * (C * paged_part_floats<D>());
+        const bool whole = x0 == 0 && x1 == cost;
+        if (!process_piece<D, ALIGNED, false>(a, rq, b, t, g, kb, ke, whole, part, smem_raw))
+            process_piece<D, ALIGNED, true>(a, rq, b, t, g, kb, ke, whole, part, smem_raw);
+        u += x1 - x0;
+        if (plan.whole || u >= end) return;
+    }
+}
+
+// blockIdx.x = item x Hkv + KV head, blockIdx.y = row group: joins the pieces of an item that fell to several workgroups, in their order.
+template <int D>
+__global__ __launch_bounds__(256) void paged_tile_join_kernel(const PagedArgs a) {
+    const int g = blockIdx.x % a.Hkv;
+    int64_t item = blockIdx.x / a.Hkv;
+    const TilePlan plan = tile_plan(a, 0, 0);
+    if (plan.whole || plan.total == 0) return;
+    int64_t start = 0;   // of the request's units
+    int b = 0;
+    PagedRequest rq{0, 0, 0};
+    TileCosts c{0, 0, 0};
+    for (; b < a.B; ++b) {
+        rq = paged_request(a, b);
+        if (rq.n == 0) continue;
+        c = tile_costs(a, rq);
+        if (item < c.n_ct) break;
+        item -= c.n_ct;
+        start += c.before(c.n_ct);
+    }
+    if (b == a.B) return;
+    const int t = (int)item;
+    const int64_t u0 = start + c.before(t);
+    const int w0 = paged_owner(u0, plan.total, plan.sharers), w1 = paged_owner(u0 + c.tile(t) - 1, plan.total, plan.sharers), n = w1 - w0 + 1;
+    if (n == 1) return;   // whole: stored already
+    constexpr int SH = D / 4;   // dims of a thread
+    const int cl = 64 * blockIdx.y + threadIdx.x / 4, e0 = 4 * (threadIdx.x % 4);
+    TileItem<D> it;
+    it.init(a, rq, t, g);
+    if (it.col0 + cl >= it.cols) return;
+    float top = PAGED_NO_MAX, l = 0.f;
+    f32x4 o[SH / 4];
+#pragma unroll
+    for (int i = 0; i < SH / 4; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < n; ++i) {
+        const float* part = a.partials + (((size_t)(w0 + i) * a.Hkv + g) * 2 + (i == 0 ? 1 : 0)) * (C * paged_part_floats<D>());
+        const float pm = part[2 * cl], pl = part[2 * cl + 1];
+        if (pl == 0.f) continue;   // (the piece saw nothing of this column; it may hold anything)
+        const float up = fmaxf(top, pm), f = __builtin_amdgcn_exp2f(top - up), w = __builtin_amdgcn_exp2f(pm - up);
+        top = up;
+        l = l * f + pl * w;
+#pragma unroll
+        for (int k = 0; k < SH / 4; ++k) o[k] = o[k] * f + *reinterpret_cast<const f32x4*>(part + 2 * C + cl * D + 16 * k + e0) * w;
+    }
+    const bool none = l == 0.f;
+    const float inv_l = none ? 0.f : 1.0f / l;
+    const size_t oc = it.out_row(a, cl);
+    typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
+#pragma unroll
+    for (int k = 0; k < SH / 4; ++k) {
+        bf16x4 y;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = (__bf16)(o[k][e] * inv_l);
+        *reinterpret_cast<bf16x4*>((__bf16*)a.out + oc * D + 16 * k + e0) = y;
+    }
+    if (e0 == 0 && a.lse != nullptr) a.lse[oc] = none ? -INFINITY : (top + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+}
+
+template <int D, bool ALIGNED>
+hipError_t launch(const PagedArgs& a, hipStream_t st) {
+    static_assert(tile_lds_bytes<D>() <= 160 * 1024, "LDS of a compute unit");
+    // Raises the kernel's dynamic LDS limit, once per process.
+    static const hipError_t once = hipFuncSetAttribute(reinterpret_cast<const void*>(&paged_tile_kernel<D, ALIGNED>),
+                                                       hipFuncAttributeMaxDynamicSharedMemorySize, (int)tile_lds_bytes<D>());
+    if (once != hipSuccess) return once;
+    // no more items than this: full tiles of all rows, and one that is not full per request
+    const int64_t rows = std::min<int64_t>(a.T, (int64_t)a.B * a.max_new);
+    const int64_t items = rows * a.G / C + std::min<int64_t>(a.B, rows * a.G / (a.cols_lo + 1));
+    const int64_t grid = std::max<int64_t>(a.n_wg, items);
+    paged_tile_kernel<D, ALIGNED><<<dim3((unsigned)(grid * a.Hkv)), dim3(64 * WAVES), tile_lds_bytes<D>(), st>>>(a);
+    paged_tile_join_kernel<D><<<dim3((unsigned)(items * a.Hkv), RG), dim3(256), 0, st>>>(a);
+    return hipGetLastError();
+}
+
+int tile_workgroups(int Hkv, int n_cu) { return std::max(1, n_cu / Hkv); }   // per KV head
+
+}  // namespace
+
+size_t paged_tile_partials_bytes(const Shape& s, int n_cu) {
+    return (size_t)tile_workgroups(s.Hkv, n_cu) * s.Hkv * 2 * C * (s.d + 2) * sizeof(float);
+}
+
+hipError_t launch_paged_tile(const Shape& s, const PagedArgs& args, int n_cu, hipStream_t st) {
+    PagedArgs a = args;
+    a.n_wg = tile_workgroups(s.Hkv, n_cu);
+    if (s.d == 128) return a.P % RW == 0 ? launch<128, true>(a, st) : launch<128, false>(a, st);
+    return a.P % RW == 0 ? launch<64, true>(a, st) : launch<64, false>(a, st);
+}
+
+}  // namespace fr

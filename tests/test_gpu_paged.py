@@ -203,6 +203,21 @@ def test_attention(layer, form):
     ctx.close()
 
 
+@pytest.mark.parametrize("layer", ["g4", "g2_d64", "f32_d64"])
+@pytest.mark.parametrize("form", ["decode", "one_long", "verify", "mixed", "long_chunk"])
+def test_what_an_earlier_call_left_in_the_workspace(layer, form):
+    """Partial results of a batch that is NaN throughout lie where the next call's go: nothing of them is read."""
+    ctx = make_ctx(LAYERS[layer])
+    for lens in ([(900, 1)] * 40, [(1000, 300), (500, 200)], [(6000, 1)], [(3000, 70)]):
+        nan = make_batch(LAYERS[layer], lens, 16, seed=1)
+        nan["kp"][:], nan["vp"][:] = np.nan, np.nan
+        run_attn(ctx, nan)
+    bt = make_batch(LAYERS[layer], FORMS[form], 16, seed=3)
+    out, lse = run_attn(ctx, bt)
+    check_attn(bt, out, lse, None if len(bt["q"]) < 60 else set(range(0, len(bt["q"]), 13)) | {len(bt["q"]) - 1} | {131, 132, 133})
+    ctx.close()
+
+
 @pytest.mark.parametrize("page", [1, 2, 3, 5, 8, 12, 16, 20, 31, 100, 256, 5000])
 @pytest.mark.parametrize("layer", ["g4", "g2_d64", "f32_d64"])
 def test_page_sizes(layer, page):
