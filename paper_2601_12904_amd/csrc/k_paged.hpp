@@ -43,15 +43,14 @@ __device__ __forceinline__ int paged_position(const PagedArgs& a, const PagedReq
 __device__ __forceinline__ int paged_token(const PagedArgs& a, int col) { return a.G > 1 ? (int)__umulhi((uint32_t)col, a.g_magic) : col; }
 __device__ __forceinline__ int paged_block(const PagedArgs& a, int j) { return (int)(__umulhi(2u * (uint32_t)j, a.p_magic) >> a.p_shift); }
 
-__device__ __forceinline__ int64_t wave_sum64(int64_t v) {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
+// Over the first n lanes of the wave (lanes 0 .. n - 1 hold the result; the others hold nothing of use): a batch of few requests takes few steps.
+__device__ __forceinline__ int64_t wave_sum64(int64_t v, int n) {
+    for (int d = 1; d < n; d <<= 1) v += __shfl_xor(v, d);
     return v;
 }
-__device__ __forceinline__ int64_t wave_scan64(int64_t v) {   // inclusive
+__device__ __forceinline__ int64_t wave_scan64(int64_t v, int n) {   // inclusive
     const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
+    for (int d = 1; d < n; d <<= 1) {
         const int64_t t = __shfl_up(v, d);
         if (lane >= d) v += t;
     }
@@ -64,8 +63,13 @@ __device__ __forceinline__ int64_t uniform64(int64_t v) {
 
 // How a launch's work is dealt out.  The work of a KV head is one line of units: requests in order, of each its column tiles, of each its units of keys.
 // Workgroup w of n takes units floor(w U / n) .. floor((w + 1) U / n) - 1 of it, wherever they begin and end, so every workgroup has the same
-// share whatever the lengths are, and the host need not know them.  n is at most U (paged_sharers): none of them goes without.  An item (column tile) that falls to several workgroups leaves a partial result
+// share whatever the lengths are, and the host need not know them.  n is at most U (paged_sharers): none of them goes without.  Every item that is cut
+// is cut at the first unit of some workgroup, so a joining pass has one candidate per workgroup, however many items there are.  An item (column tile) that falls to several workgroups leaves a partial result
 // per piece: in slot 2 w of a workgroup whose piece begins behind the item's start, in 2 w + 1 of the one that has its start but not its end.
+// blockIdx.x = workgroup of the KV head x Hkv + KV head: blocks go to the eight dies in turn, so that with 8 KV heads each die's cache serves one of them.
+__device__ __forceinline__ int paged_head(const PagedArgs& a) { return blockIdx.x % a.Hkv; }
+__device__ __forceinline__ int paged_workgroup(const PagedArgs& a) { return blockIdx.x / a.Hkv; }
+inline unsigned paged_grid(int64_t workgroups, int Hkv) { return (unsigned)(workgroups * Hkv); }
 struct PagedLine {
     int64_t total;    // U
     int64_t start;    // of the unit that was looked for: first unit of its request
@@ -79,13 +83,13 @@ __device__ __forceinline__ PagedLine paged_line(int B, Cost cost, Find find) {
     int64_t mine = 0;
     for (int b0 = 0; b0 < B; b0 += 64) {
         mine = b0 + lane < B ? cost(b0 + lane) : 0;
-        r.total += uniform64(wave_sum64(mine));
+        r.total += uniform64(wave_sum64(mine, min(64, B - b0)));
     }
     const int64_t u = find(r.total);
     if (u < 0 || u >= r.total) return r;
     for (int b0 = 0; b0 < B; b0 += 64) {
         if (B > 64) mine = b0 + lane < B ? cost(b0 + lane) : 0;
-        const int64_t upto = r.start + wave_scan64(mine);
+        const int64_t upto = r.start + wave_scan64(mine, min(64, B - b0));
         const uint64_t beyond = __ballot(upto > u);
         if (beyond != 0) {
             const int l = __builtin_ctzll(beyond);
@@ -99,8 +103,16 @@ __device__ __forceinline__ PagedLine paged_line(int B, Cost cost, Find find) {
     return r;
 }
 __device__ __forceinline__ int paged_sharers(const PagedArgs& a, int64_t total) { return (int)min((int64_t)a.n_wg, total); }
-__device__ __forceinline__ int64_t paged_first_unit(int64_t w, int64_t total, int n) { return w * total / n; }
-__device__ __forceinline__ int paged_owner(int64_t u, int64_t total, int n) { return (int)(((u + 1) * n - 1) / total); }   // the workgroup that has unit u
+// floor(x / d), x >= 0, d > 0: by a product in fp64 and a step or two (a division of 64-bit integers is over a hundred instructions; eight of them were 4 us in front of
+// a piece's first load).
+__device__ __forceinline__ int64_t paged_div(int64_t x, int64_t d) {
+    int64_t q = (int64_t)((double)x * (1.0 / (double)d));
+    while (q * d > x) --q;
+    while ((q + 1) * d <= x) ++q;
+    return q;
+}
+__device__ __forceinline__ int64_t paged_first_unit(int64_t w, int64_t total, int n) { return paged_div(w * total, n); }
+__device__ __forceinline__ int paged_owner(int64_t u, int64_t total, int n) { return (int)paged_div((u + 1) * n - 1, total); }   // the workgroup that has unit u
 
 // ---- matrix-core helpers ------------------------------------------------------------------------------
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
@@ -141,6 +153,16 @@ __device__ __forceinline__ void paged_copy16(const void* src, uint32_t lds) {   
 __device__ __forceinline__ void paged_copy4(const void* src, uint32_t lds) {    // lane i's 4 bytes to lds + 4 i
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(src), "s"(__builtin_amdgcn_readfirstlane(lds)) : "memory");
 }
+// The same from a base that the wave shares.
+__device__ __forceinline__ void paged_copy16(const void* base, uint32_t off, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(off), "s"(base), "s"(__builtin_amdgcn_readfirstlane(lds)) : "memory");
+}
+__device__ __forceinline__ void paged_copy4(const void* base, uint32_t off, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" : : "v"(off), "s"(base), "s"(__builtin_amdgcn_readfirstlane(lds)) : "memory");
+}
+__device__ __forceinline__ const unsigned char* paged_uniform(const unsigned char* p) {   // in scalar registers, whatever the compiler makes of it
+    return reinterpret_cast<const unsigned char*>((uintptr_t)uniform64((int64_t)(uintptr_t)p));
+}
 template <int N>
 __device__ __forceinline__ void paged_wait_but() {   // until all but the wave's last N copies have landed
     static_assert(N < 16, "one field of the counter");
@@ -154,6 +176,13 @@ hipError_t launch_paged_stream(const Shape& s, const PagedArgs& a, int n_cu, hip
 
 size_t paged_tile_partials_bytes(const Shape& s, int n_cu);
 hipError_t launch_paged_tile(const Shape& s, const PagedArgs& a, int n_cu, hipStream_t st);
+
+__device__ __forceinline__ void paged_lds_barrier() {   // a workgroup's barrier for LDS alone: __syncthreads() also waits for stores to memory
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
 
 // ---- joining pieces -----------------------------------------------------------------------------------
 // A piece's slot: [column][D + 2] fp32: exponent reference (base 2), sum of weights, weighted values.

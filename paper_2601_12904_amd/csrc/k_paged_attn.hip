@@ -120,13 +120,16 @@ hipError_t launch_paged_attn(const Shape& s, const PagedAttnArgs& args, float* p
         a.cols_hi = INT32_MAX;
         return s.d == 128 ? launch_rows<float, 128>(a, st) : launch_rows<float, 64>(a, st);
     }
-    // requests with few columns, and the others
+    // requests with few columns, and the others (a few of the former beside others: with them, two launches less)
     const int few = std::max(64, s.G);
+    const bool others = (int64_t)args.max_new * s.G > few;
     a.cols_lo = 0;
     a.cols_hi = few;
-    hipError_t e = launch_paged_stream(s, a, n_cu, st);
-    if (e != hipSuccess || (int64_t)args.max_new * s.G <= few) return e;
-    a.cols_lo = few;
+    if (!others || args.n_requests > 8) {
+        hipError_t e = launch_paged_stream(s, a, n_cu, st);
+        if (e != hipSuccess || !others) return e;
+        a.cols_lo = few;
+    }
     a.cols_hi = INT32_MAX;
     if (const char* m = getenv("PAGED_MODE")) a.split_mode = atoi(m);
     return launch_paged_tile(s, a, n_cu, st);

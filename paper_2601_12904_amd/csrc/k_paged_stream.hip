@@ -289,7 +289,7 @@ struct StreamPiece {
                         }
                 }
         }
-        __syncthreads();   // everyone is done with the copies
+        paged_lds_barrier();   // everyone is done with the copies
         // ---- merge the waves ---------------------------------------------------------------------------------------------
 #pragma unroll
         for (int nb = 0; nb < NC; ++nb) {
@@ -302,7 +302,7 @@ struct StreamPiece {
                     *reinterpret_cast<f32x4*>(&sm.o[wave][16 * nb + x][NJ * (4 * kg + v) + 4 * h]) =
                         f32x4{o[4 * h][nb][v], o[4 * h + 1][nb][v], o[4 * h + 2][nb][v], o[4 * h + 3][nb][v]};
         }
-        __syncthreads();
+        paged_lds_barrier();
         constexpr int NV = D / 8;
         for (int i = tid; i < C * NV; i += 64 * W) {
             const int c = i / NV, v8 = i % NV, n = col0 + c;
@@ -337,17 +337,16 @@ struct StreamPiece {
             *reinterpret_cast<u32x4*>((__bf16*)a.out + oc * D + 8 * v8) = __builtin_bit_cast(u32x4, y);
             if (v8 == 0 && a.lse != nullptr) a.lse[oc] = none ? -INFINITY : (top + __builtin_amdgcn_logf(lsum)) * 0.6931471805599453f;
         }
-        __syncthreads();   // (the next piece's copies overwrite what was merged)
+        paged_lds_barrier();   // (the next piece's copies overwrite what was merged)
     }
 };
 
-// blockIdx.x = workgroup w of the KV head x Hkv + KV head.
 template <int D, int NC, bool ALIGNED>
 __global__ __launch_bounds__(64 * W, 2) void paged_stream_kernel(const PagedArgs a) {
     extern __shared__ __attribute__((aligned(16))) unsigned char smem_raw[];
     auto& sm = *reinterpret_cast<StreamLds<D, NC>*>(smem_raw);
     constexpr int C = 16 * NC;
-    const int g = blockIdx.x % a.Hkv, w = blockIdx.x / a.Hkv;
+    const int g = paged_head(a), w = paged_workgroup(a);
     int64_t u = 0, end = 0;
     const PagedLine line = paged_line(a.B, [&](int b) { return stream_cost<C>(a, b); }, [&](int64_t total) {
         const int n = paged_sharers(a, total);
@@ -365,10 +364,10 @@ __global__ __launch_bounds__(64 * W, 2) void paged_stream_kernel(const PagedArgs
         if (cost == 0) continue;
         while (u < end && u < start + cost) {
             const int64_t in = u - start;
-            const int ct = (int)(in / units), r0 = (int)(in - (int64_t)ct * units);
+            const int ct = (int)paged_div(in, units), r0 = (int)(in - (int64_t)ct * units);
             const int r1 = (int)min((int64_t)units, r0 + (end - u));
             const bool whole = r0 == 0 && r1 == units;
-            float* part = a.partials + ((size_t)blockIdx.x * 2 + (r0 > 0 ? 0 : 1)) * (C * paged_part_floats<D>());
+            float* part = a.partials + (((size_t)w * a.Hkv + g) * 2 + (r0 > 0 ? 0 : 1)) * (C * paged_part_floats<D>());
             StreamPiece<D, NC, ALIGNED>::run(a, sm, rq, b, ct, g, r0, r1, whole, part);
             u += r1 - r0;
         }
@@ -376,79 +375,86 @@ __global__ __launch_bounds__(64 * W, 2) void paged_stream_kernel(const PagedArgs
     }
 }
 
-// One workgroup per (request, column tile, KV head): joins the pieces of an item that fell to several workgroups, in their order.
+// Joins the pieces of the items that fell to several workgroups, in their order: blockIdx.x = (workgroup - 1) x Hkv + KV head; that workgroup's first unit, if it is the
+// first cut of an item, stands for it.  One wave per column (blockIdx.y: four of them), all of a column's pieces in one or two trips to memory.
 template <int D, int NC>
-__global__ __launch_bounds__(256) void paged_stream_join_kernel(const PagedArgs a, int max_ct) {
-    constexpr int C = 16 * NC, PF = paged_part_floats<D>();
-    const int g = blockIdx.x % a.Hkv, ct = blockIdx.x / a.Hkv % max_ct, b = blockIdx.x / a.Hkv / max_ct;
+__global__ __launch_bounds__(256) void paged_stream_join_kernel(const PagedArgs a) {
+    constexpr int C = 16 * NC, PF = paged_part_floats<D>(), EPT = D / 64, AHEAD = 16;
+    const int g = blockIdx.x % a.Hkv, cut = blockIdx.x / a.Hkv + 1;
+    int64_t u = 0;
+    int sharers = 0;
+    const PagedLine line = paged_line(a.B, [&](int b) { return stream_cost<C>(a, b); }, [&](int64_t total) {
+        sharers = paged_sharers(a, total);
+        if (cut >= sharers) return (int64_t)-1;
+        u = paged_first_unit(cut, total, sharers);
+        return u;
+    });
+    if (line.b < 0) return;
     int n_ct, units;
     PagedRequest rq;
-    const int64_t cost = stream_cost<C>(a, b, &n_ct, &units, &rq);
-    if (cost == 0 || ct >= n_ct) return;
-    int64_t before = 0, all = 0;
-    const int lane = threadIdx.x & 63;
-    for (int b0 = 0; b0 < a.B; b0 += 64) {
-        const int64_t c = b0 + lane < a.B ? stream_cost<C>(a, b0 + lane) : 0;
-        all += uniform64(wave_sum64(c));
-        before += uniform64(wave_sum64(b0 + lane < b ? c : 0));
-    }
-    const int64_t u0 = before + (int64_t)ct * units;
-    const int sharers = paged_sharers(a, all), w0 = paged_owner(u0, all, sharers), w1 = paged_owner(u0 + units - 1, all, sharers);
-    if (w0 == w1) return;   // whole: stored already
-    const int cols = min(C, rq.n * a.G - C * ct), n = w1 - w0 + 1;
-    auto piece = [&](int i) { return a.partials + (((size_t)(w0 + i) * a.Hkv + g) * 2 + (i == 0 ? 1 : 0)) * (C * PF); };
-    for (int idx = threadIdx.x; idx < cols * D; idx += 256) {
-        const int c = idx / D, e = idx % D;
-        float top = PAGED_NO_MAX, l = 0.f, o = 0.f;
-        constexpr int AHEAD = 8;
-        for (int i0 = 0; i0 < n; i0 += AHEAD) {
-            float pm[AHEAD], pl[AHEAD], po[AHEAD];
+    stream_cost<C>(a, line.b, &n_ct, &units, &rq);
+    const int ct = (int)paged_div(u - line.start, units);
+    const int64_t u0 = line.start + (int64_t)ct * units;   // the item's first unit
+    if (u == u0 || paged_owner(u0, line.total, sharers) != cut - 1) return;
+    const int w0 = cut - 1, n = paged_owner(u0 + units - 1, line.total, sharers) - w0 + 1;
+    const int c = 4 * blockIdx.y + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if (c >= min(C, rq.n * a.G - C * ct)) return;
+    float top = PAGED_NO_MAX, l = 0.f, o[EPT];
 #pragma unroll
-            for (int k = 0; k < AHEAD; ++k) {   // (past the end: the last piece, which does not count)
-                const float* p = piece(min(i0 + k, n - 1)) + c * PF;
-                pm[k] = p[0];
-                pl[k] = p[1];
-                po[k] = p[2 + e];
-            }
-            float up = top;
+    for (int e = 0; e < EPT; ++e) o[e] = 0.f;
+    for (int i0 = 0; i0 < n; i0 += AHEAD) {
+        float pm[AHEAD], pl[AHEAD], po[AHEAD][EPT];
 #pragma unroll
-            for (int k = 0; k < AHEAD; ++k) up = i0 + k < n ? fmaxf(up, pm[k]) : up;
-            const float f = __builtin_amdgcn_exp2f(top - up);
-            top = up;
-            l *= f;
-            o *= f;
+        for (int k = 0; k < AHEAD; ++k) {   // (past the end: the last piece, which does not count)
+            const int i = min(i0 + k, n - 1);
+            const float* p = a.partials + (((size_t)(w0 + i) * a.Hkv + g) * 2 + (i == 0 ? 1 : 0)) * (C * PF) + c * PF;
+            pm[k] = p[0];
+            pl[k] = p[1];
 #pragma unroll
-            for (int k = 0; k < AHEAD; ++k) {
-                if (i0 + k >= n) continue;
-                const float w = __builtin_amdgcn_exp2f(pm[k] - top);
-                l += pl[k] * w;
-                o += po[k] * w;
-            }
+            for (int e = 0; e < EPT; ++e) po[k][e] = p[2 + EPT * lane + e];
         }
-        const int col = C * ct + c, i = paged_token(a, col);
-        const size_t oc = (size_t)(rq.first + i) * a.Hq + g * a.G + (col - i * a.G);
-        const bool none = l == 0.f;
-        ((__bf16*)a.out)[oc * D + e] = (__bf16)(none ? 0.f : o * (1.0f / l));
-        if (e == 0 && a.lse != nullptr) a.lse[oc] = none ? -INFINITY : (top + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+        float up = top;
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) up = i0 + k < n ? fmaxf(up, pm[k]) : up;
+        const float f = __builtin_amdgcn_exp2f(top - up);
+        top = up;
+        l *= f;
+#pragma unroll
+        for (int e = 0; e < EPT; ++e) o[e] *= f;
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            if (i0 + k >= n) continue;
+            const float w = __builtin_amdgcn_exp2f(pm[k] - top);
+            l += pl[k] * w;
+#pragma unroll
+            for (int e = 0; e < EPT; ++e) o[e] += po[k][e] * w;
+        }
     }
+    const int col = C * ct + c, i = paged_token(a, col);
+    const size_t oc = (size_t)(rq.first + i) * a.Hq + g * a.G + (col - i * a.G);
+    const bool none = l == 0.f;
+    const float inv_l = none ? 0.f : 1.0f / l;
+#pragma unroll
+    for (int e = 0; e < EPT; ++e) ((__bf16*)a.out)[oc * D + EPT * lane + e] = (__bf16)(o[e] * inv_l);
+    if (lane == 0 && a.lse != nullptr) a.lse[oc] = none ? -INFINITY : (top + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
 template <int D, int NC, bool ALIGNED>
-hipError_t launch(const PagedArgs& a, int max_ct, hipStream_t st) {
+hipError_t launch(const PagedArgs& a, int cols, hipStream_t st) {
     using Lds = StreamLds<D, NC>;
     static_assert(sizeof(Lds) <= 80 * 1024, "two workgroups per compute unit");
     // Raises the kernel's dynamic LDS limit, once per process.
     static const hipError_t once = hipFuncSetAttribute(reinterpret_cast<const void*>(&paged_stream_kernel<D, NC, ALIGNED>),
                                                        hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Lds));
     if (once != hipSuccess) return once;
-    paged_stream_kernel<D, NC, ALIGNED><<<dim3((unsigned)(a.n_wg * a.Hkv)), dim3(64 * W), sizeof(Lds), st>>>(a);
-    if (a.n_wg > 1) paged_stream_join_kernel<D, NC><<<dim3((unsigned)(a.B * max_ct * a.Hkv)), dim3(256), 0, st>>>(a, max_ct);
+    paged_stream_kernel<D, NC, ALIGNED><<<dim3(paged_grid(a.n_wg, a.Hkv)), dim3(64 * W), sizeof(Lds), st>>>(a);
+    if (a.n_wg > 1) paged_stream_join_kernel<D, NC><<<dim3((unsigned)((a.n_wg - 1) * a.Hkv), (unsigned)((cols + 3) / 4)), dim3(256), 0, st>>>(a);
     return hipGetLastError();
 }
 
 template <int D, int NC>
-hipError_t launch(const PagedArgs& a, int max_ct, hipStream_t st) {
-    return a.P % StreamPiece<D, NC, true>::COPIES == 0 ? launch<D, NC, true>(a, max_ct, st) : launch<D, NC, false>(a, max_ct, st);
+hipError_t launch(const PagedArgs& a, int cols, hipStream_t st) {
+    return a.P % StreamPiece<D, NC, true>::COPIES == 0 ? launch<D, NC, true>(a, cols, st) : launch<D, NC, false>(a, cols, st);
 }
 
 }  // namespace
@@ -462,9 +468,9 @@ hipError_t launch_paged_stream(const Shape& s, const PagedArgs& args, int n_cu, 
     a.n_wg = std::max(1, 2 * n_cu / s.Hkv);   // two per compute unit are resident
     const int64_t most = std::min<int64_t>((int64_t)a.max_new * s.G, a.cols_hi);
     const int nc = most <= 16 ? 1 : 2;
-    const int max_ct = (int)((most + 16 * nc - 1) / (16 * nc));
-    if (s.d == 128) return nc == 1 ? launch<128, 1>(a, max_ct, st) : launch<128, 2>(a, max_ct, st);
-    return nc == 1 ? launch<64, 1>(a, max_ct, st) : launch<64, 2>(a, max_ct, st);
+    const int cols = (int)std::min<int64_t>(most, 16 * nc);   // of a tile
+    if (s.d == 128) return nc == 1 ? launch<128, 1>(a, cols, st) : launch<128, 2>(a, cols, st);
+    return nc == 1 ? launch<64, 1>(a, cols, st) : launch<64, 2>(a, cols, st);
 }
 
 }  // namespace fr

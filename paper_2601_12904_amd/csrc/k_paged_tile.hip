@@ -37,7 +37,7 @@ namespace {
 constexpr int WAVES = 8, RG = 4, KT = 64, NC = 4;   // waves; row groups; keys of a tile; blocks of 16 columns of a row group
 constexpr int C = 64 * RG;                          // columns of a tile
 constexpr int RW = KT / WAVES;                      // rows of a tile that a wave brings
-constexpr int TILE0 = 4;                            // ring slot of tile 0's page numbers
+constexpr int TILE0 = 8;                            // ring slot of tile 0's page numbers; the others: tile % 8
 constexpr int ITEM_KEYS = 192;                      // what a piece costs beside its keys, in keys (prologue, joining of the waves, output)
 
 typedef short __attribute__((ext_vector_type(4))) i16x4;
@@ -51,18 +51,20 @@ struct __attribute__((aligned(16))) TileLds {
     unsigned char k[3][TILE], v[3][TILE];                     // rings
     unsigned char q[QL > 0 ? RG * QL * NC * 1024 : 16];
     int pos[RG][64];                                          // positions of the columns (masked tiles)
-    int page[WAVES][5][64];                                   // page numbers of the rows that a wave is to bring, per tile
-    unsigned char hole[5][8];                                 // per tile and wave: bit r = its row r has no page
+    int page[WAVES][9][64];                                   // page numbers of the rows that a wave is to bring, per tile
+    unsigned char hole[8][8];                                 // per tile and wave: bit r = its row r has no page (EXACT)
     float ref[WAVES][64];                                     // the waves' largest logits (EXACT)
     int apart;
 };
 template <int D>
 constexpr int EXCHANGE_WAVE = D / 32 * NC * 1024 + 1024;      // half of a wave's accumulators, and its sums
 template <int D>
-constexpr size_t tile_lds_bytes() {
+constexpr size_t references_at() {   // behind everything: the columns' exponent references (registers would spill)
     constexpr size_t a = sizeof(TileLds<D>), b = (size_t)WAVES * EXCHANGE_WAVE<D>, c = (size_t)RG * 64 * (D + 8) * 2;
     return a > b ? (a > c ? a : c) : (b > c ? b : c);
 }
+template <int D>
+constexpr size_t tile_lds_bytes() { return references_at<D>() + C * sizeof(float) + 2 * WAVES * sizeof(int); }   // and the waves' answers to two questions
 
 // ---- how the work is dealt out --------------------------------------------------------------------------
 // The cost of a column tile in keys: what its last row sees, about (the line of work only has to be the same for everybody), and what every item takes.
@@ -115,11 +117,11 @@ __device__ __forceinline__ TilePlan tile_plan(const PagedArgs& a, int64_t item, 
                 least = min(least, c.tile(0));
             }
         }
-        total += uniform64(wave_sum64(cost));
-        items += uniform64(wave_sum64(n_ct));
+        const int lanes = min(64, a.B - b0);
+        total += uniform64(wave_sum64(cost, lanes));
+        items += uniform64(wave_sum64(n_ct, lanes));
     }
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
+    for (int d = 1; d < min(64, a.B); d <<= 1) {
         most = max(most, (int64_t)__shfl_xor(most, d));
         least = min(least, (int64_t)__shfl_xor(least, d));
     }
@@ -128,9 +130,9 @@ __device__ __forceinline__ TilePlan tile_plan(const PagedArgs& a, int64_t item, 
     TilePlan p{false, total, 1, -1, 0};
     if (total == 0) return p;
     const int n = p.sharers = paged_sharers(a, total);
-    const int64_t share = total / n;
+    const int64_t share = paged_div(total, n);
     const int64_t in_items = items <= n ? most : max(most, share + least);
-    p.whole = a.split_mode == 1 || (a.split_mode == 0 && in_items <= share + share / 10 + 2 * ITEM_KEYS);
+    p.whole = a.split_mode == 1 || (a.split_mode == 0 && in_items <= share + (share >> 3) + 2 * ITEM_KEYS);
     const int64_t u = p.whole ? item : paged_first_unit(w, total, n);
     if (p.whole ? u >= items : w >= n) return p;
     for (int b0 = 0; b0 < a.B; b0 += 64) {
@@ -146,7 +148,7 @@ __device__ __forceinline__ TilePlan tile_plan(const PagedArgs& a, int64_t item, 
                 }
             }
         }
-        const int64_t mine = p.whole ? n_ct : cost, upto = p.start + wave_scan64(mine);
+        const int64_t mine = p.whole ? n_ct : cost, upto = p.start + wave_scan64(mine, min(64, a.B - b0));
         const uint64_t beyond = __ballot(upto > u);
         if (beyond != 0) {
             const int l = __builtin_ctzll(beyond);
@@ -160,6 +162,17 @@ __device__ __forceinline__ TilePlan tile_plan(const PagedArgs& a, int64_t item, 
 }
 
 __device__ __forceinline__ f32x4 mfma(const bf16x8& a, const bf16x8& b, const f32x4& c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+
+// A barrier (for LDS), and whether any thread says v; uniform in the compiler's eyes too (what lies behind a divergent branch keeps its registers through the other side).
+__device__ __forceinline__ bool any_of_workgroup(bool v, int* answers) {
+    const bool any = __any(v);
+    if ((threadIdx.x & 63) == 0) answers[threadIdx.x >> 6] = any ? 1 : 0;
+    paged_lds_barrier();
+    int all = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) all |= answers[w];
+    return __builtin_amdgcn_readfirstlane(all) != 0;
+}
 
 // A column tile of a request, and what a lane knows of its columns.
 template <int D>
@@ -192,11 +205,12 @@ struct TileItem {
 
 // One matrix phase: O^T += V^T P^T for the wave's half of one tile, S^T = K Q^T for its half of another.  tv, tk: LDS addresses of the lane's first fragments.
 // Fragments are requested PF steps of four matrix instructions ahead.
+// m: the columns' references, for the softmax phase behind it.
 template <int D, bool PV>
 __device__ __forceinline__ void matrix_phase(uint32_t tv, uint32_t tk, const bf16x8 (&qf)[NC][TileLds<D>::QR], uint32_t q_lds, const u32x4 (&p)[NC],
-                                             f32x4 (&o)[D / 16][NC], f32x4 (&s)[2][NC]) {
+                                             f32x4 (&o)[D / 16][NC], f32x4 (&s)[2][NC], uint32_t ref_lds, f32x4& m) {
     using L = TileLds<D>;
-    constexpr int NK = L::NK, MD = L::MD, PF = 4, QR = L::QR, FIRST = PV ? 0 : MD, STEPS = MD + 2 * NK, BLOCK = 16 * L::ROW;
+    constexpr int NK = L::NK, MD = L::MD, PF = 5, QR = L::QR, FIRST = PV ? 0 : MD, STEPS = MD + 2 * NK, BLOCK = 16 * L::ROW;
     auto dims = [](int j) { return QR < NK ? (j & 1 ? j / 2 : QR + j / 2) : j; };   // order of the dims: LDS, registers, LDS, registers
     bf16x8 fr[PF + 1], qb[2][NC];
     const lds_b128 q_frag = reinterpret_cast<lds_b128>((uintptr_t)q_lds);
@@ -217,6 +231,7 @@ __device__ __forceinline__ void matrix_phase(uint32_t tv, uint32_t tk, const bf1
     };
     int reads[STEPS] = {};   // LDS reads issued in front of step i's products
     __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int i = FIRST; i < FIRST + PF; ++i) fr[i % (PF + 1)] = frag(i);
     if (!PV) reads[FIRST] += load_q(0);
@@ -228,6 +243,10 @@ __device__ __forceinline__ void matrix_phase(uint32_t tv, uint32_t tk, const bf1
         }
         if (PV && i == MD - 2) reads[i] += load_q(0);   // two steps ahead
         if (i >= MD && (i - MD) % 2 == 0 && (i - MD) / 2 + 1 < NK) reads[i] += load_q((i - MD) / 2 + 1);
+        if (PV && i == STEPS - 3) {
+            m = *reinterpret_cast<const f32x4 __attribute__((address_space(3)))*>((uintptr_t)ref_lds);
+            ++reads[i];
+        }
         const bf16x8 f = fr[i % (PF + 1)];
         if (i < MD) {
 #pragma unroll
@@ -254,6 +273,7 @@ __device__ __forceinline__ void matrix_phase(uint32_t tv, uint32_t tk, const bf1
         if (reads[i] == NC + 2) __builtin_amdgcn_sched_group_barrier(0x100, NC + 2, 0);
         __builtin_amdgcn_sched_group_barrier(0x008, NC, 0);
     }
+    __builtin_amdgcn_s_setprio(0);
     __builtin_amdgcn_sched_barrier(0);
 }
 
@@ -282,27 +302,26 @@ __device__ __forceinline__ bool process_piece(const PagedArgs& a, const PagedReq
     }
     const uint32_t k_base = paged_lds(sm.k[0]), v_base = paged_lds(sm.v[0]);
     const uint32_t q_lds = paged_lds(sm.q) + group * (QL * NC * 1024) + lane * 16u;
-    bf16x8 qf[NC][QR];
-    {
-        bf16x8 ql[2][QL > 0 ? QL : 1];
+    bf16x8 qf[NC][QR], ql[2][QL > 0 ? QL : 1];
 #pragma unroll
-        for (int nb = 0; nb < NC; ++nb) {
-            const __bf16* p = (const __bf16*)a.q + it.out_row(a, 64 * group + 16 * nb + x) * D + 8 * kg;
+    for (int nb = 0; nb < NC; ++nb) {
+        const __bf16* p = (const __bf16*)a.q + it.out_row(a, 64 * group + 16 * nb + x) * D + 8 * kg;
 #pragma unroll
-            for (int ks = 0; ks < QR; ++ks) qf[nb][ks] = *reinterpret_cast<const bf16x8*>(p + 32 * ks);
-        }
+        for (int ks = 0; ks < QR; ++ks) qf[nb][ks] = *reinterpret_cast<const bf16x8*>(p + 32 * ks);
+    }
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {   // the two waves of a row group bring two column blocks' each to LDS
-            const __bf16* p = (const __bf16*)a.q + it.out_row(a, 64 * group + 16 * (2 * second + i) + x) * D + 8 * kg;
+    for (int i = 0; i < 2; ++i) {   // the two waves of a row group bring two column blocks' each to LDS
+        const __bf16* p = (const __bf16*)a.q + it.out_row(a, 64 * group + 16 * (2 * second + i) + x) * D + 8 * kg;
 #pragma unroll
-            for (int ks = 0; ks < QL; ++ks) ql[i][ks] = *reinterpret_cast<const bf16x8*>(p + 32 * (QR + ks));
-        }
+        for (int ks = 0; ks < QL; ++ks) ql[i][ks] = *reinterpret_cast<const bf16x8*>(p + 32 * (QR + ks));
+    }
+    auto store_q = [&] {
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int ks = 0; ks < QL; ++ks)
                 *reinterpret_cast<bf16x8 __attribute__((address_space(3)))*>((uintptr_t)(q_lds + (ks * NC + 2 * second + i) * 1024)) = ql[i][ks];
-    }
+    };
     if (!second) {
         int token, head;
         it.column(a, 64 * group + lane, &token, &head);
@@ -314,33 +333,40 @@ __device__ __forceinline__ bool process_piece(const PagedArgs& a, const PagedReq
     const int32_t* table = a.block_table + (size_t)b * a.W;
     const uint32_t row_bytes = (uint32_t)(a.Hkv * D * 2);
     const unsigned char *k_pages = (const unsigned char*)a.k_pages + (size_t)g * ROW, *v_pages = (const unsigned char*)a.v_pages + (size_t)g * ROW;
+    const uint64_t page_bytes = (uint64_t)(uint32_t)a.P * row_bytes;
     const uint32_t page_lds = paged_lds(sm.page[wave]);
     auto is_page = [&](int p) { return (uint32_t)p < (uint32_t)a.n_pages; };
     const int last = max(ke - 1, 0);   // (past the piece's last tile the copies repeat that one: the counts of the waits stay the same, and nobody reads them)
-    auto copy_pages = [&](int kt, int slot) {    // page numbers of the wave's rows of tile kt
-        const int j = KT * min(kt, last) + RW * wave + (lane & (RW - 1));
-        paged_copy4(table + paged_block(a, max(min(j, p_last), 0)), page_lds + 256 * slot);
+    auto copy_pages = [&](int kt, int slot) {    // page numbers of the wave's rows of tile kt (aligned pages: one, in every lane)
+        const int j = KT * min(kt, last) + RW * wave;
+        if constexpr (ALIGNED)
+            paged_copy4(paged_uniform((const unsigned char*)(table + paged_block(a, min(j, p_last)))), 0u, page_lds + 256 * slot);
+        else
+            paged_copy4(table + paged_block(a, min(j + (lane & (RW - 1)), p_last)), page_lds + 256 * slot);
     };
-    // Where the wave's rows of a tile are: aligned pages: byte offset of the first one, the same for all lanes, and how many rows there are before the last
-    // visible one; else the row of each copy's lane.
+    // Where the wave's rows of a tile are.  Aligned pages: the first one, the same for all lanes, and how many rows there are behind it up to the last visible
+    // one (those behind that repeat it); else the row of each copy's lane.
     struct Rows {
         uint64_t at;
         int most;
-        uint32_t row[COPIES];
+        uint32_t row[ALIGNED ? 1 : COPIES];
     };
-    auto swz = [](int r) { return D == 128 ? r & 15 : r >> 1 & 7; };
+    // Place of vector v of row r: v ^ swz(r).  The 16 rows of a K fragment meet in no bank, and neither do the 32-byte pieces that a transposing read
+    // takes from 8 consecutive rows.
+    auto swz = [](int r) { return D == 128 ? (r & 7) << 1 | (r >> 3 & 1) : (r >> 1 & 3) << 1 | (r >> 3 & 1); };
     const int lr = lane / RV, lv = lane % RV;   // row of the lane within a copy, place of its vector
     auto lane_vec = [&](int c) { return 16u * (uint32_t)(lv ^ swz(RW * wave + RC * c + lr)); };
+    const uint32_t lane_off = (uint32_t)lr * row_bytes + lane_vec(0);   // (copy 1: rows RC .. of the eight, whose vectors are permuted by 8 more)
+    static_assert(COPIES == 1 || (COPIES == 2 && RC == 4), "swz(r + 4) = swz(r) ^ 8");
     auto find_rows = [&](int kt, int slot) {
         Rows r;
         const int j0 = KT * min(kt, last) + RW * wave;
         int holes;
         if constexpr (ALIGNED) {
             const int page = __builtin_amdgcn_readfirstlane(sm.page[wave][slot][0]), jc = min(j0, p_last);
-            holes = is_page(page) ? 0 : (1 << RW) - 1;
-            r.at = ((uint64_t)(holes ? 0 : page) * (uint32_t)a.P + (uint32_t)(jc - paged_block(a, jc) * a.P)) * row_bytes;
-            r.most = p_last - jc;       // (rows behind it repeat it)
-            if (j0 > p_last) r.most = 0;
+            holes = !EXACT || is_page(page) ? 0 : (1 << RW) - 1;   // (else the piece has none)
+            r.at = (uint64_t)(uint32_t)(holes ? 0 : page) * page_bytes + (uint64_t)(uint32_t)(jc - paged_block(a, jc) * a.P) * row_bytes;
+            r.most = j0 > p_last ? 0 : p_last - jc;
         } else {
             const int mine = sm.page[wave][slot][lane & (RW - 1)];
             holes = (int)(__ballot(!is_page(mine)) & ((1 << RW) - 1));
@@ -350,23 +376,32 @@ __device__ __forceinline__ bool process_piece(const PagedArgs& a, const PagedReq
                 r.row[c] = (uint32_t)(is_page(page) ? page : 0) * (uint32_t)a.P + (uint32_t)(j - paged_block(a, j) * a.P);
             }
         }
-        if (lane == 0) sm.hole[slot][wave] = (unsigned char)holes;
+        if (EXACT && lane == 0) sm.hole[slot & 7][wave] = (unsigned char)holes;
         return r;
     };
     auto copy_rows = [&](const Rows& r, const unsigned char* pages, uint32_t lds) {
+        if constexpr (ALIGNED) {
+            const unsigned char* src = pages + r.at;
+            const uint32_t to = lds + RW * wave * ROW;
+            if (__builtin_expect(r.most >= RW - 1, 1)) {
+                paged_copy16(src, lane_off, to);
+                if constexpr (COPIES == 2) paged_copy16(src + RC * row_bytes, lane_off ^ 128u, to + 1024);
+            } else {
 #pragma unroll
-        for (int c = 0; c < COPIES; ++c) {
-            const unsigned char* src;
-            if constexpr (ALIGNED) src = pages + r.at + (size_t)((uint32_t)min(RC * c + lr, r.most) * row_bytes) + lane_vec(c);
-            else src = pages + (size_t)r.row[c] * row_bytes + lane_vec(c);
-            paged_copy16(src, lds + (RW * wave + RC * c) * ROW);
+                for (int c = 0; c < COPIES; ++c) paged_copy16(src, (uint32_t)min(RC * c + lr, r.most) * row_bytes + lane_vec(c), to + 1024 * c);
+            }
+        } else {
+#pragma unroll
+            for (int c = 0; c < COPIES; ++c) paged_copy16(pages + (size_t)r.row[c] * row_bytes + lane_vec(c), lds + (RW * wave + RC * c) * ROW);
         }
     };
     f32x4 o[MD][NC], s[2][NC];
     u32x4 p[NC];
-    float l[NC], m[NC];
-#pragma unroll
-    for (int nb = 0; nb < NC; ++nb) m[nb] = PAGED_NO_MAX;
+    float l[NC];
+    float* refs = reinterpret_cast<float*>(smem_raw + references_at<D>()) + 64 * group + 4 * x;   // of the lane's four columns
+    const uint32_t ref_lds = paged_lds(smem_raw + references_at<D>()) + 256 * group + 16 * x;
+    int* answers = reinterpret_cast<int*>(smem_raw + references_at<D>() + C * sizeof(float));
+    f32x4 m;
     const int n_plain = (it.p_first + 1) / KT;   // leading tiles whose keys are visible to every column
     if (!empty) {
         const uint32_t tk0 = k_base + x * ROW + 16 * (kg ^ swz(x)), tk = tk0 + 32 * second * ROW;
@@ -374,18 +409,20 @@ __device__ __forceinline__ bool process_piece(const PagedArgs& a, const PagedReq
         const uint32_t tv = v_base + 32 * second * ROW + y * ROW + 16 * ((x >> 1 & 1) ^ swz(y)) + 8 * (x & 1);
         int c0, c1, c2;     // ring slots (their bytes) of tiles kt, kt + 1, kt + 2
         Rows next;          // of the tile whose values are to be copied next
-        // K tiles kb and kb + 1 and V tile kb land in LDS, the page numbers of the two behind them are on their way.
-        auto prime = [&](bool values) {
-            paged_wait_but<0>();   // (nothing that the compiler counts is in flight from here on)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) copy_pages(kb + i, (kb + i) & 3);
-            paged_wait_but<2>();
-            const Rows r0 = find_rows(kb, kb & 3);
+        auto copy_first = [&](bool values) {   // K tiles kb and kb + 1 and V tile kb
+            const Rows r0 = find_rows(kb, kb & 7);
             copy_rows(r0, k_pages, k_base);
             if (values) copy_rows(r0, v_pages, v_base);
-            next = find_rows(kb + 1, (kb + 1) & 3);
+            next = find_rows(kb + 1, (kb + 1) & 7);
             copy_rows(next, k_pages, k_base + TILE);
             c0 = 0; c1 = TILE; c2 = 2 * TILE;
+        };
+        auto prime = [&](bool values) {   // the same with the page numbers, up to those of tile kb + 4, in front
+            paged_wait_but<0>();   // (nothing that the compiler counts is in flight from here on)
+#pragma unroll
+            for (int i = 0; i < 5; ++i) copy_pages(kb + i, (kb + i) & 7);
+            paged_wait_but<3>();
+            copy_first(values);
         };
         auto mask = [&](int kt, uint32_t hole) {   // hole: bits of the wave's 32 keys
             int ln = lane;
@@ -404,7 +441,7 @@ __device__ __forceinline__ bool process_piece(const PagedArgs& a, const PagedReq
             }
         };
         auto holes_of = [&](int kt, uint32_t* mine) {   // does the tile have any, and which of the wave's 32 keys
-            const uint64_t hole = *reinterpret_cast<const uint64_t*>(sm.hole[kt & 3]);
+            const uint64_t hole = *reinterpret_cast<const uint64_t*>(sm.hole[kt & 7]);
             const uint32_t lo = __builtin_amdgcn_readfirstlane((int)(uint32_t)hole), hi = __builtin_amdgcn_readfirstlane((int)(hole >> 32));
             *mine = second ? hi : lo;
             return (lo | hi) != 0;
@@ -415,20 +452,22 @@ __device__ __forceinline__ bool process_piece(const PagedArgs& a, const PagedReq
             asm volatile("" ::: "memory");
         };
         if constexpr (EXACT) {   // the maximum of its logits over the piece's visible keys
+            f32x4 top = {PAGED_NO_MAX, PAGED_NO_MAX, PAGED_NO_MAX, PAGED_NO_MAX};
+            store_q();
             prime(false);
             paged_wait_but<0>();
             __syncthreads();
             for (int kt = kb; kt < ke; ++kt) {   // K tiles kt and kt + 1 are in ring slots, kt + 2 follows
-                const Rows after = find_rows(kt + 2, (kt + 2) & 3);
+                const Rows after = find_rows(kt + 2, (kt + 2) & 7);
                 copy_rows(after, k_pages, k_base + c2);
-                copy_pages(kt + 4, kt & 3);
-                matrix_phase<D, false>(0, tk + c0, qf, q_lds, p, o, s);
+                copy_pages(kt + 5, (kt + 5) & 7);
+                matrix_phase<D, false>(0, tk + c0, qf, q_lds, p, o, s, ref_lds, m);
                 uint32_t hole;
                 if (holes_of(kt, &hole) || kt >= n_plain) mask(kt, hole);
 #pragma unroll
                 for (int nb = 0; nb < NC; ++nb)
 #pragma unroll
-                    for (int v = 0; v < 4; ++v) m[nb] = fmaxf(m[nb], fmaxf(s[0][nb][v], s[1][nb][v]));
+                    for (int v = 0; v < 4; ++v) top[nb] = fmaxf(top[nb], fmaxf(s[0][nb][v], s[1][nb][v]));
                 paged_wait_but<COPIES + 1>();          // all but the newest tile
                 __builtin_amdgcn_s_waitcnt(0xc07f);    // lgkmcnt(0): the wave's own reads and writes
                 plain_barrier();
@@ -437,29 +476,40 @@ __device__ __forceinline__ bool process_piece(const PagedArgs& a, const PagedReq
             }
 #pragma unroll
             for (int nb = 0; nb < NC; ++nb) {
-                m[nb] = paged_column_max(m[nb]);
-                if (kg == 0) sm.ref[wave][16 * nb + x] = m[nb];
+                top[nb] = paged_column_max(top[nb]);
+                if (kg == 0) sm.ref[wave][16 * nb + x] = top[nb];
             }
             paged_wait_but<0>();
             __syncthreads();
 #pragma unroll
             for (int nb = 0; nb < NC; ++nb) {
-                const float top = fmaxf(m[nb], sm.ref[wave ^ 4][16 * nb + x]);
-                m[nb] = top == PAGED_NO_MAX ? PAGED_NO_MAX : top * a.scale_log2e;
+                const float t = fmaxf(top[nb], sm.ref[wave ^ 4][16 * nb + x]);
+                if (!second && kg == 0) refs[nb] = t == PAGED_NO_MAX ? PAGED_NO_MAX : t * a.scale_log2e;
             }
             prime(true);
+#pragma unroll
+            for (int i = 0; i < TILE / (64 * WAVES * 16); ++i)
+                *reinterpret_cast<u32x4*>(sm.v[2] + (i * 64 * WAVES + tid) * 16) = u32x4{0u, 0u, 0u, 0u};
             paged_wait_but<0>();
             __syncthreads();
         } else {   // the maximum over the visible ones of keys 0..31
-            paged_wait_but<0>();
+            // (positions without a page, in tile 0 or in the piece: EXACT sees to them)
             copy_pages(0, TILE0);
-            paged_wait_but<0>();
+#pragma unroll
+            for (int i = 0; i < 5; ++i) copy_pages(kb + i, (kb + i) & 7);
+            bool none = tid <= min(KT - 1, p_last) && !is_page(table[paged_block(a, min(tid, p_last))]);
+            for (int i = paged_block(a, KT * kb) + tid; i <= paged_block(a, min(KT * ke - 1, p_last)); i += 64 * WAVES) none = none || !is_page(table[i]);
+            store_q();
+#pragma unroll
+            for (int i = 0; i < TILE / (64 * WAVES * 16); ++i)   // V ring slot 2 holds zeros for the matrix phase in front
+                *reinterpret_cast<u32x4*>(sm.v[2] + (i * 64 * WAVES + tid) * 16) = u32x4{0u, 0u, 0u, 0u};
+            paged_wait_but<0>();   // (nothing that the compiler counts is in flight from here on)
+            if (any_of_workgroup(none, answers)) return false;
             copy_rows(find_rows(0, TILE0), k_pages, k_base + 2 * TILE);
-            prime(true);
+            copy_first(true);
             paged_wait_but<0>();
-            __syncthreads();
-            if (*reinterpret_cast<const uint32_t*>(sm.hole[TILE0]) != 0) return false;   // (uniform; behind the barrier nothing is in flight)
-            matrix_phase<D, false>(0, tk0 + 2 * TILE, qf, q_lds, p, o, s);
+            paged_lds_barrier();
+            matrix_phase<D, false>(0, tk0 + 2 * TILE, qf, q_lds, p, o, s, ref_lds, m);
 #pragma unroll
             for (int nb = 0; nb < NC; ++nb) {
                 const int pos = sm.pos[group][16 * nb + x];
@@ -468,14 +518,11 @@ __device__ __forceinline__ bool process_piece(const PagedArgs& a, const PagedReq
                 for (int bb = 0; bb < 2; ++bb)
 #pragma unroll
                     for (int v = 0; v < 4; ++v) t = fmaxf(t, 16 * bb + 4 * kg + v <= pos ? s[bb][nb][v] : -INFINITY);
-                m[nb] = fmaxf(paged_column_max(t) * a.scale_log2e, PAGED_NO_MAX);
+                t = fmaxf(paged_column_max(t) * a.scale_log2e, PAGED_NO_MAX);
+                if (!second && kg == 0) refs[nb] = t;
             }
-            __syncthreads();   // (K ring slot 2 is free)
+            paged_lds_barrier();   // (K ring slot 2 is free)
         }
-#pragma unroll
-        for (int i = 0; i < TILE / (64 * WAVES * 16); ++i)   // V ring slot 2 holds zeros for the matrix phase in front
-            *reinterpret_cast<u32x4*>(sm.v[2] + (i * 64 * WAVES + tid) * 16) = u32x4{0u, 0u, 0u, 0u};
-        __syncthreads();
 #pragma unroll
         for (int nb = 0; nb < NC; ++nb) {
             l[nb] = 0.f;
@@ -486,18 +533,18 @@ __device__ __forceinline__ bool process_piece(const PagedArgs& a, const PagedReq
 
         // ---- tile loop -------------------------------------------------------------------------------------
         // Barrier kt says that K tile kt and V tile kt - 1 have landed and that nobody reads K tile kt - 1 and V tile kt - 2 any more; the copies
-        // behind it refill those slots: K tile kt + 2 and V tile kt + 1; and the page numbers of tile kt + 4.
+        // behind it refill those slots: K tile kt + 2 and V tile kt + 1; and the page numbers of tile kt + 5.
         int vp = 2 * TILE;                      // ring slot of V tile kt - 1
+        Rows after = find_rows(kb + 2, (kb + 2) & 7);   // of tile kt + 2, found during the softmax phase in front of copies(kt)
         auto copies = [&](int kt) {
-            const Rows after = find_rows(kt + 2, (kt + 2) & 3);
             copy_rows(after, k_pages, k_base + c2);
             copy_rows(next, v_pages, v_base + c1);
-            copy_pages(kt + 4, kt & 3);
+            copy_pages(kt + 5, (kt + 5) & 7);
             next = after;
         };
         // Values of tile kt (ring slot `slot`), this wave's rows, that are not finite: out of LDS.
         auto scrub = [&](int kt, int slot) {
-            if (kt < n_plain && sm.hole[kt & 3][wave] == 0) return;   // (its own entry)
+            if (kt < n_plain && sm.hole[kt & 7][wave] == 0) return;   // (its own entry)
             bool found = false;
 #pragma unroll 1
             for (int i = lane * 16; i < RW * ROW; i += 1024) {
@@ -523,21 +570,23 @@ __device__ __forceinline__ bool process_piece(const PagedArgs& a, const PagedReq
             c0 = c1; c1 = c2; c2 = vp;
             __builtin_amdgcn_sched_barrier(0);
         };
-        auto softmax = [&](int kt) {
-            uint32_t hole;
-            const bool any_hole = holes_of(kt, &hole);
+        auto softmax = [&](int kt, int copied) {
+            after = find_rows(copied + 3, (copied + 3) & 7);
+            uint32_t hole = 0;
+            bool any_hole = false;
+            if constexpr (EXACT) any_hole = holes_of(kt, &hole);
             if (__builtin_expect(kt >= n_plain || any_hole, 0)) mask(kt, hole);
 #pragma unroll
             for (int nb = 0; nb < NC; ++nb) {
-                float s0 = 0.f, s1 = 0.f;
+                float s0, s1;
 #pragma unroll
                 for (int bb = 0; bb < 2; ++bb)
 #pragma unroll
                     for (int v = 0; v < 4; v += 2) {
                         const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[bb][nb][v], a.scale_log2e, -m[nb]));
                         const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[bb][nb][v + 1], a.scale_log2e, -m[nb]));
-                        s0 += p0;
-                        s1 += p1;
+                        s0 = bb == 0 && v == 0 ? p0 : s0 + p0;
+                        s1 = bb == 0 && v == 0 ? p1 : s1 + p1;
                         bf16x2 w;
                         w[0] = (__bf16)p0;
                         w[1] = (__bf16)p1;
@@ -549,24 +598,26 @@ __device__ __forceinline__ bool process_piece(const PagedArgs& a, const PagedReq
         };
         if (!second) {
             for (int kt = kb;; ++kt) {
-                matrix_phase<D, true>(tv + vp, tk + c0, qf, q_lds, p, o, s);
+                matrix_phase<D, true>(tv + vp, tk + c0, qf, q_lds, p, o, s, ref_lds, m);
                 if (kt == ke) break;
                 copies(kt);
-                softmax(kt);
+                softmax(kt, kt);
                 barrier(kt);
             }
         } else {
             copies(kb);
+            after = find_rows(kb + 3, (kb + 3) & 7);
             for (int kt = kb;; ++kt) {
-                matrix_phase<D, true>(tv + vp, tk + c0, qf, q_lds, p, o, s);
+                matrix_phase<D, true>(tv + vp, tk + c0, qf, q_lds, p, o, s, ref_lds, m);
                 if (kt == ke) break;
                 barrier(kt);
                 copies(kt + 1);
-                softmax(kt);
+                softmax(kt, kt + 1);
             }
         }
         paged_wait_but<0>();
     } else {
+        if (tid < C) reinterpret_cast<float*>(smem_raw + references_at<D>())[tid] = PAGED_NO_MAX;
 #pragma unroll
         for (int nb = 0; nb < NC; ++nb) {
             l[nb] = 0.f;
@@ -576,11 +627,11 @@ __device__ __forceinline__ bool process_piece(const PagedArgs& a, const PagedReq
     }
 
     // ---- the two waves of a row group add up: each keeps half of the dims ------------------------------------------
-    __syncthreads();   // (also: everyone is done with the rings)
+    paged_lds_barrier();   // (also: everyone is done with the rings)
     bool apart = false;
     if constexpr (EXACT) {
         apart = sm.apart != 0;
-        __syncthreads();
+        paged_lds_barrier();
     }
     constexpr int MH = MD / 2;
     f32x4 oh[MH][NC];
@@ -602,7 +653,7 @@ __device__ __forceinline__ bool process_piece(const PagedArgs& a, const PagedReq
                 *reinterpret_cast<f32x4*>(mine + (md * NC + nb) * 1024) = w;
             }
         *reinterpret_cast<f32x4*>(mine + MH * NC * 1024) = f32x4{l[0], l[1], l[2], l[3]};
-        __syncthreads();
+        paged_lds_barrier();
 #pragma unroll
         for (int md = 0; md < MH; ++md)
 #pragma unroll
@@ -660,16 +711,15 @@ __device__ __forceinline__ bool process_piece(const PagedArgs& a, const PagedReq
                 for (int v = 0; v < 4; ++v) check += fabsf(oh[md][nb][v]);
             bad = bad || !(check < limit);
         }
-        bad = __builtin_amdgcn_readfirstlane(__syncthreads_or(bad ? 1 : 0)) != 0;   // (also: the exchange has been read)
-        if (bad) return false;
+        if (any_of_workgroup(bad, answers + WAVES)) return false;   // (also: the exchange has been read)
     } else {
-        __syncthreads();
+        paged_lds_barrier();
     }
     if (!whole) {
 #pragma unroll
         for (int nb = 0; nb < NC; ++nb) {
             const int c = 64 * group + 16 * nb + x;
-            if (!second && kg == 0) { part[2 * c] = m[nb]; part[2 * c + 1] = l[nb]; }
+            if (!second && kg == 0) { part[2 * c] = refs[nb]; part[2 * c + 1] = l[nb]; }
 #pragma unroll
             for (int md = 0; md < MH; ++md) *reinterpret_cast<f32x4*>(part + 2 * C + c * D + 16 * (md0 + md) + 4 * kg) = oh[md][nb];
         }
@@ -692,28 +742,27 @@ __device__ __forceinline__ bool process_piece(const PagedArgs& a, const PagedReq
         }
         const int cl = 64 * group + 16 * nb + x;
         if (!second && kg == 0 && a.lse != nullptr && it.col0 + cl < it.cols)
-            a.lse[it.out_row(a, cl)] = none ? -INFINITY : (m[nb] + __builtin_amdgcn_logf(l[nb])) * 0.6931471805599453f;
+            a.lse[it.out_row(a, cl)] = none ? -INFINITY : (refs[nb] + __builtin_amdgcn_logf(l[nb])) * 0.6931471805599453f;
     }
-    __syncthreads();   // (the rows of a group come from both of its waves)
+    paged_lds_barrier();   // (the rows of a group come from both of its waves)
 #pragma unroll
     for (int i = 0; i < NV / 2; ++i) {
         const int c = (64 / NV) * (i + second * (NV / 2)) + lane / NV, v = lane % NV;
         if (it.col0 + 64 * group + c < it.cols)
             *reinterpret_cast<u32x4*>((__bf16*)a.out + it.out_row(a, 64 * group + c) * D + 8 * v) = *reinterpret_cast<const u32x4*>(&ob[c * PITCH + 8 * v]);
     }
-    __syncthreads();   // (the next piece's copies overwrite what was staged)
+    paged_lds_barrier();   // (the next piece's copies overwrite what was staged)
     return true;
 }
 
-// blockIdx.x = (item, or workgroup of the line) x Hkv + KV head: with 8 KV heads each die's cache serves one of them.
 template <int D, bool ALIGNED>
 __global__ __launch_bounds__(64 * WAVES) void paged_tile_kernel(const PagedArgs a) {
     extern __shared__ __attribute__((aligned(16))) unsigned char smem_raw[];
-    const int g = blockIdx.x % a.Hkv, w = blockIdx.x / a.Hkv;
+    const int g = paged_head(a), w = paged_workgroup(a);
     const TilePlan plan = tile_plan(a, w, w);
     if (plan.b < 0) return;
-    int64_t u = paged_first_unit(w, plan.total, plan.sharers), start = plan.start;
-    const int64_t end = paged_first_unit(w + 1, plan.total, plan.sharers);
+    int64_t u = plan.whole ? 0 : paged_first_unit(w, plan.total, plan.sharers), start = plan.start;
+    const int64_t end = plan.whole ? 0 : paged_first_unit(w + 1, plan.total, plan.sharers);
     for (int b = plan.b; b < a.B;) {
         const PagedRequest rq = paged_request(a, b);
         const TileCosts c = tile_costs(a, rq);
@@ -727,8 +776,8 @@ __global__ __launch_bounds__(64 * WAVES) void paged_tile_kernel(const PagedArgs 
         const int i = (int64_t)C * (t + 1) >= (int64_t)rq.n * a.G ? rq.n - 1 : (C * (t + 1) - 1) / a.G;   // the tile's last row
         const int n = (paged_position(a, rq, i) + KT) / KT;                                              // its key tiles
         const int64_t cost = c.tile(t), x0 = plan.whole ? 0 : u - start - c.before(t), x1 = plan.whole ? cost : min(cost, x0 + (end - u));
-        const int kb = (int)(x0 * n / cost), ke = (int)(x1 * n / cost);
-        float* part = a.partials + ((size_t)blockIdx.x * 2 + (x0 > 0 ? 0 : 1)) * (C * paged_part_floats<D>());
+        const int kb = x0 == 0 ? 0 : (int)paged_div(x0 * n, cost), ke = x1 == cost ? n : (int)paged_div(x1 * n, cost);
+        float* part = a.partials + (((size_t)w * a.Hkv + g) * 2 + (x0 > 0 ? 0 : 1)) * (C * paged_part_floats<D>());
         const bool whole = x0 == 0 && x1 == cost;
         if (!process_piece<D, ALIGNED, false>(a, rq, b, t, g, kb, ke, whole, part, smem_raw))
             process_piece<D, ALIGNED, true>(a, rq, b, t, g, kb, ke, whole, part, smem_raw);
@@ -737,59 +786,61 @@ __global__ __launch_bounds__(64 * WAVES) void paged_tile_kernel(const PagedArgs 
     }
 }
 
-// blockIdx.x = item x Hkv + KV head, blockIdx.y = row group: joins the pieces of an item that fell to several workgroups, in their order.
+// Joins the pieces of the items that fell to several workgroups, in their order: blockIdx.x = (workgroup - 1) x Hkv + KV head; that workgroup's first unit, if it is the
+// first cut of an item, stands for it.  blockIdx.y: 16 columns, 16 threads each.
 template <int D>
 __global__ __launch_bounds__(256) void paged_tile_join_kernel(const PagedArgs a) {
-    const int g = blockIdx.x % a.Hkv;
-    int64_t item = blockIdx.x / a.Hkv;
-    const TilePlan plan = tile_plan(a, 0, 0);
-    if (plan.whole || plan.total == 0) return;
-    int64_t start = 0;   // of the request's units
-    int b = 0;
-    PagedRequest rq{0, 0, 0};
-    TileCosts c{0, 0, 0};
-    for (; b < a.B; ++b) {
-        rq = paged_request(a, b);
-        if (rq.n == 0) continue;
-        c = tile_costs(a, rq);
-        if (item < c.n_ct) break;
-        item -= c.n_ct;
-        start += c.before(c.n_ct);
-    }
-    if (b == a.B) return;
-    const int t = (int)item;
-    const int64_t u0 = start + c.before(t);
-    const int w0 = paged_owner(u0, plan.total, plan.sharers), w1 = paged_owner(u0 + c.tile(t) - 1, plan.total, plan.sharers), n = w1 - w0 + 1;
-    if (n == 1) return;   // whole: stored already
-    constexpr int SH = D / 4;   // dims of a thread
-    const int cl = 64 * blockIdx.y + threadIdx.x / 4, e0 = 4 * (threadIdx.x % 4);
+    const int g = blockIdx.x % a.Hkv, cut = blockIdx.x / a.Hkv + 1;
+    const TilePlan plan = tile_plan(a, 0, cut);
+    if (plan.whole || plan.b < 0) return;
+    const PagedRequest rq = paged_request(a, plan.b);
+    const TileCosts c = tile_costs(a, rq);
+    const int64_t u = paged_first_unit(cut, plan.total, plan.sharers);
+    const int t = c.tile_at(u - plan.start);
+    const int64_t u0 = plan.start + c.before(t);   // the item's first unit
+    if (u == u0 || paged_owner(u0, plan.total, plan.sharers) != cut - 1) return;
+    const int w0 = cut - 1, n = paged_owner(u0 + c.tile(t) - 1, plan.total, plan.sharers) - w0 + 1;
+    constexpr int NV = D / 64, AHEAD = 8;   // vectors of a thread; pieces in flight
+    const int cl = 16 * blockIdx.y + threadIdx.x / 16, e0 = 4 * (threadIdx.x % 16);
     TileItem<D> it;
     it.init(a, rq, t, g);
     if (it.col0 + cl >= it.cols) return;
     float top = PAGED_NO_MAX, l = 0.f;
-    f32x4 o[SH / 4];
+    f32x4 o[NV];
 #pragma unroll
-    for (int i = 0; i < SH / 4; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int i = 0; i < n; ++i) {
-        const float* part = a.partials + (((size_t)(w0 + i) * a.Hkv + g) * 2 + (i == 0 ? 1 : 0)) * (C * paged_part_floats<D>());
-        const float pm = part[2 * cl], pl = part[2 * cl + 1];
-        if (pl == 0.f) continue;   // (the piece saw nothing of this column; it may hold anything)
-        const float up = fmaxf(top, pm), f = __builtin_amdgcn_exp2f(top - up), w = __builtin_amdgcn_exp2f(pm - up);
-        top = up;
-        l = l * f + pl * w;
+    for (int k = 0; k < NV; ++k) o[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int i0 = 0; i0 < n; i0 += AHEAD) {
+        float pm[AHEAD], pl[AHEAD];
+        f32x4 po[AHEAD][NV];
 #pragma unroll
-        for (int k = 0; k < SH / 4; ++k) o[k] = o[k] * f + *reinterpret_cast<const f32x4*>(part + 2 * C + cl * D + 16 * k + e0) * w;
+        for (int k = 0; k < AHEAD; ++k) {   // (past the end: the last piece, which does not count)
+            const int i = min(i0 + k, n - 1);
+            const float* part = a.partials + (((size_t)(w0 + i) * a.Hkv + g) * 2 + (i == 0 ? 1 : 0)) * (C * paged_part_floats<D>());
+            pm[k] = part[2 * cl];
+            pl[k] = part[2 * cl + 1];
+#pragma unroll
+            for (int v = 0; v < NV; ++v) po[k][v] = *reinterpret_cast<const f32x4*>(part + 2 * C + cl * D + 64 * v + e0);
+        }
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            if (i0 + k >= n || pl[k] == 0.f) continue;   // (a piece that saw nothing of this column: its values may be anything)
+            const float up = fmaxf(top, pm[k]), f = __builtin_amdgcn_exp2f(top - up), w = __builtin_amdgcn_exp2f(pm[k] - up);
+            top = up;
+            l = l * f + pl[k] * w;
+#pragma unroll
+            for (int v = 0; v < NV; ++v) o[v] = o[v] * f + po[k][v] * w;
+        }
     }
     const bool none = l == 0.f;
     const float inv_l = none ? 0.f : 1.0f / l;
     const size_t oc = it.out_row(a, cl);
     typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
 #pragma unroll
-    for (int k = 0; k < SH / 4; ++k) {
+    for (int v = 0; v < NV; ++v) {
         bf16x4 y;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] = (__bf16)(o[k][e] * inv_l);
-        *reinterpret_cast<bf16x4*>((__bf16*)a.out + oc * D + 16 * k + e0) = y;
+        for (int e = 0; e < 4; ++e) y[e] = (__bf16)(o[v][e] * inv_l);
+        *reinterpret_cast<bf16x4*>((__bf16*)a.out + oc * D + 64 * v + e0) = y;
     }
     if (e0 == 0 && a.lse != nullptr) a.lse[oc] = none ? -INFINITY : (top + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
@@ -805,8 +856,8 @@ hipError_t launch(const PagedArgs& a, hipStream_t st) {
     const int64_t rows = std::min<int64_t>(a.T, (int64_t)a.B * a.max_new);
     const int64_t items = rows * a.G / C + std::min<int64_t>(a.B, rows * a.G / (a.cols_lo + 1));
     const int64_t grid = std::max<int64_t>(a.n_wg, items);
-    paged_tile_kernel<D, ALIGNED><<<dim3((unsigned)(grid * a.Hkv)), dim3(64 * WAVES), tile_lds_bytes<D>(), st>>>(a);
-    paged_tile_join_kernel<D><<<dim3((unsigned)(items * a.Hkv), RG), dim3(256), 0, st>>>(a);
+    paged_tile_kernel<D, ALIGNED><<<dim3(paged_grid(grid, a.Hkv)), dim3(64 * WAVES), tile_lds_bytes<D>(), st>>>(a);
+    if (a.n_wg > 1) paged_tile_join_kernel<D><<<dim3((unsigned)((a.n_wg - 1) * a.Hkv), C / 16), dim3(256), 0, st>>>(a);
     return hipGetLastError();
 }
 
