@@ -15,7 +15,8 @@
 // A wave alternates between a matrix phase (O += its half of tile kt - 1, logits of its half of tile kt) and a softmax phase; the two waves of a SIMD do so in turn,
 // so that the vector work of one runs beside the matrix instructions of the other:
 //   waves 0..3   barrier kt | matrix (kt - 1, kt) | copies kt | softmax kt
-//   waves 4..7   barrier kt | copies kt | softmax kt - 1 | matrix (kt - 1, kt)
+//   waves 4..7   barrier kt | softmax kt - 1 | copies kt | matrix (kt - 1, kt)
+// (copies of all waves at once, behind the barrier, hold the softmax up: 1000 cycles for five of them each, 440 apart).
 //
 // Softmax.  exp(x - m) / sum exp(x - m) does not depend on m, and fp32 and bf16 leave about 2^127 of room, so a column's exponent reference is the maximum over its
 // visible ones of the request's keys 0..31, in every piece of its item, and the loop holds no maximum, no comparison and no rescaling (which would
@@ -570,8 +571,8 @@ __device__ __forceinline__ bool process_piece(const PagedArgs& a, const PagedReq
             c0 = c1; c1 = c2; c2 = vp;
             __builtin_amdgcn_sched_barrier(0);
         };
-        auto softmax = [&](int kt, int copied) {
-            after = find_rows(copied + 3, (copied + 3) & 7);
+        auto softmax = [&](int kt, int ahead) {   // and the rows of tile `ahead`, which the copies behind it, or the next ones, do not bring yet
+            const Rows found = find_rows(ahead, ahead & 7);
             uint32_t hole = 0;
             bool any_hole = false;
             if constexpr (EXACT) any_hole = holes_of(kt, &hole);
@@ -595,13 +596,14 @@ __device__ __forceinline__ bool process_piece(const PagedArgs& a, const PagedReq
                 l[nb] += s0 + s1;
             }
             __builtin_amdgcn_sched_barrier(0);
+            return found;
         };
         if (!second) {
             for (int kt = kb;; ++kt) {
                 matrix_phase<D, true>(tv + vp, tk + c0, qf, q_lds, p, o, s, ref_lds, m);
                 if (kt == ke) break;
                 copies(kt);
-                softmax(kt, kt);
+                after = softmax(kt, kt + 3);
                 barrier(kt);
             }
         } else {
@@ -611,8 +613,9 @@ __device__ __forceinline__ bool process_piece(const PagedArgs& a, const PagedReq
                 matrix_phase<D, true>(tv + vp, tk + c0, qf, q_lds, p, o, s, ref_lds, m);
                 if (kt == ke) break;
                 barrier(kt);
+                const Rows found = softmax(kt, kt + 4);
                 copies(kt + 1);
-                softmax(kt, kt + 1);
+                after = found;
             }
         }
         paged_wait_but<0>();
