@@ -19,7 +19,6 @@ struct PagedArgs {
     uint32_t g_magic;        // ceil(2^32 / G): c / G = mulhi(c, g_magic) for c < 2^26
     uint32_t p_magic, p_shift;   // j / P = mulhi(2 j, p_magic) >> p_shift for j < 2^30
     float scale_log2e;
-    int split_mode;
 };
 
 // A request as a launch sees it.

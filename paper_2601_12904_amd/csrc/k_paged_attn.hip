@@ -6,7 +6,6 @@
 #include "k_paged.hpp"
 
 #include <algorithm>
-#include <cstdlib>
 
 namespace fr {
 
@@ -131,7 +130,6 @@ hipError_t launch_paged_attn(const Shape& s, const PagedAttnArgs& args, float* p
         a.cols_lo = few;
     }
     a.cols_hi = INT32_MAX;
-    if (const char* m = getenv("PAGED_MODE")) a.split_mode = atoi(m);
     return launch_paged_tile(s, a, n_cu, st);
 }
 

@@ -39,7 +39,8 @@ constexpr int WAVES = 8, RG = 4, KT = 64, NC = 4;   // waves; row groups; keys o
 constexpr int C = 64 * RG;                          // columns of a tile
 constexpr int RW = KT / WAVES;                      // rows of a tile that a wave brings
 constexpr int TILE0 = 8;                            // ring slot of tile 0's page numbers; the others: tile % 8
-constexpr int ITEM_KEYS = 192;                      // what a piece costs beside its keys, in keys (prologue, joining of the waves, output)
+constexpr int ITEM_KEYS = 512;                      // what a piece costs beside its keys, in keys: 13 us of prologue, joining of the waves and output, a tile 1.5 us
+constexpr int MIN_SHARE = 1024;                     // a share smaller than this costs more to write and read as partial results than it saves
 
 typedef short __attribute__((ext_vector_type(4))) i16x4;
 typedef const bf16x8 __attribute__((address_space(3)))* lds_b128;
@@ -100,7 +101,9 @@ struct TilePlan {
 };
 // Both ways of dealing: whole items, longest of a request first, which walk the keys of a KV head side by side and share them in the caches; or equal shares.
 // Whole where its estimated end (the longest item; the average load and one of the shortest, where there are several items for each workgroup) is no later than that of
-// equal shares, which read keys at different places (a tenth) and join pieces.
+// equal shares, which read keys at different places (an eighth) and join pieces (three items' own cost).  us whole : in shares, 32 / 8 heads, rows behind
+// positions: 2048 behind 14336 455 : 469, 1024 361 : 267, 512 344 : 178, 64 333 : 76; 2048 behind 4000 197 : 237, 512 137 : 115; 300 behind 1000 66 : 86; from nothing
+// 512 49 : 80, 4096 182 : 259, 8192 544 : 713; 2300 behind 4000 280 : 254, 2400 behind 14000 736 : 569; 16 times 40 behind 3000 126 : 117, behind 100 61 : 115.
 __device__ __forceinline__ TilePlan tile_plan(const PagedArgs& a, int64_t item, int w) {
     const int lane = threadIdx.x & 63;
     int64_t total = 0, items = 0, cost = 0, most = 0, least = INT64_MAX;
@@ -130,10 +133,10 @@ __device__ __forceinline__ TilePlan tile_plan(const PagedArgs& a, int64_t item, 
     least = uniform64(least);
     TilePlan p{false, total, 1, -1, 0};
     if (total == 0) return p;
-    const int n = p.sharers = paged_sharers(a, total);
+    const int n = p.sharers = (int)max((int64_t)1, min((int64_t)a.n_wg, paged_div(total, MIN_SHARE)));
     const int64_t share = paged_div(total, n);
     const int64_t in_items = items <= n ? most : max(most, share + least);
-    p.whole = a.split_mode == 1 || (a.split_mode == 0 && in_items <= share + (share >> 3) + 2 * ITEM_KEYS);
+    p.whole = in_items <= share + (share >> 3) + 3 * ITEM_KEYS;
     const int64_t u = p.whole ? item : paged_first_unit(w, total, n);
     if (p.whole ? u >= items : w >= n) return p;
     for (int b0 = 0; b0 < a.B; b0 += 64) {
@@ -642,19 +645,23 @@ __device__ __forceinline__ bool process_piece(const PagedArgs& a, const PagedReq
     {
         unsigned char* mine = smem_raw + (size_t)wave * EXCHANGE_WAVE<D> + lane * 16;
         const unsigned char* other = smem_raw + (size_t)(wave ^ 4) * EXCHANGE_WAVE<D> + lane * 16;
+        if (second) {
 #pragma unroll
-        for (int md = 0; md < MH; ++md)
+            for (int md = 0; md < MH; ++md)
 #pragma unroll
-            for (int nb = 0; nb < NC; ++nb) {
-                f32x4 w;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {   // (element by element: a choice between the arrays' places would put them into memory)
-                    const float lo = o[md][nb][e], hi = o[MH + md][nb][e];
-                    w[e] = second ? lo : hi;
-                    oh[md][nb][e] = second ? hi : lo;
+                for (int nb = 0; nb < NC; ++nb) {
+                    *reinterpret_cast<f32x4*>(mine + (md * NC + nb) * 1024) = o[md][nb];
+                    oh[md][nb] = o[MH + md][nb];
                 }
-                *reinterpret_cast<f32x4*>(mine + (md * NC + nb) * 1024) = w;
-            }
+        } else {
+#pragma unroll
+            for (int md = 0; md < MH; ++md)
+#pragma unroll
+                for (int nb = 0; nb < NC; ++nb) {
+                    *reinterpret_cast<f32x4*>(mine + (md * NC + nb) * 1024) = o[MH + md][nb];
+                    oh[md][nb] = o[md][nb];
+                }
+        }
         *reinterpret_cast<f32x4*>(mine + MH * NC * 1024) = f32x4{l[0], l[1], l[2], l[3]};
         paged_lds_barrier();
 #pragma unroll
