@@ -135,12 +135,15 @@ __device__ __forceinline__ float paged_column_max(float v) {
     r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
-__device__ __forceinline__ uint32_t paged_finite_or_zero(uint32_t w) {   // the two bf16 numbers of a word, 0 in the place of one that is not finite
-    if ((w & 0x00007F80u) == 0x00007F80u) w &= 0xFFFF0000u;
-    if ((w & 0x7F800000u) == 0x7F800000u) w &= 0x0000FFFFu;
+// Is what a word holds (two bf16 numbers, or one of fp32) not finite, and the word with 0 in the place of such a number.
+template <typename T>
+__device__ __forceinline__ bool paged_not_finite(uint32_t w) { return (sizeof(T) == 2 && (w & 0x00007F80u) == 0x00007F80u) || (w & 0x7F800000u) == 0x7F800000u; }
+template <typename T>
+__device__ __forceinline__ uint32_t paged_finite_or_zero(uint32_t w) {
+    if (sizeof(T) == 2 && (w & 0x00007F80u) == 0x00007F80u) w &= 0xFFFF0000u;
+    if ((w & 0x7F800000u) == 0x7F800000u) w &= sizeof(T) == 2 ? 0x0000FFFFu : 0u;
     return w;
 }
-__device__ __forceinline__ bool paged_not_finite(uint32_t w) { return (w & 0x00007F80u) == 0x00007F80u || (w & 0x7F800000u) == 0x7F800000u; }
 
 // ---- copies global -> LDS without registers; completion: the issuing wave's vmcnt, in order of issue ------
 __device__ __forceinline__ uint32_t paged_lds(const void* p) {
@@ -164,9 +167,9 @@ __device__ __forceinline__ const unsigned char* paged_uniform(const unsigned cha
 }
 template <int N>
 __device__ __forceinline__ void paged_wait_but() {   // until all but the wave's last N copies have landed
-    static_assert(N < 16, "one field of the counter");
+    static_assert(N < 64, "the counter's six bits, in two fields");
     asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt(0x0f70 | N);
+    __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 15) | N >> 4 << 14);
     asm volatile("" ::: "memory");
 }
 

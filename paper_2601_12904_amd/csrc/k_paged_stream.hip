@@ -1,14 +1,16 @@
-// Attention over a paged cache, requests with few query columns (decoding, drafted tokens): bf16, head_dim 64 or 128.
+// Attention over a paged cache: bf16 requests with few query columns (decoding, drafted tokens), and all requests in fp32; head_dim 64 or 128.
 //
 // Every byte of K and V is used for a handful of columns, so the rate of memory is the bound.  One workgroup = one KV head x 16 NC query columns
 // ((row, query head) pairs, the heads of the group fastest); its four waves deal the blocks of 32 keys among themselves, each with accumulators of its own
 // that are merged through LDS at the end of a piece: nothing in the loop waits for another wave.  The line of work is dealt out in equal shares
 // (k_paged.hpp).
 //
-// S^T = K Q^T and O^T = V^T P^T with v_mfma_f32_16x16x32_bf16, keys on the register dimension of S^T and columns on lanes: the accumulators of two 16-key
+// S^T = K Q^T and O^T = V^T P^T with v_mfma_f32_16x16x32_bf16 (fp32: v_mfma_f32_16x16x4_f32), keys on the register dimension of S^T and columns on lanes: the accumulators of two 16-key
 // blocks are, after conversion, the B operand of the second product.  Row m of value product md is dim D / 16 m + md, so that a lane needs 16 (8)
 // neighbouring bytes of each of its eight value rows and transposes them itself with byte permutes.  Weights go into the second product as bf16 (half a
-// step, 2^-8, of each; their sum is taken in fp32 before), as the output does.
+// step, 2^-8, of each; their sum is taken in fp32 before), as the output does; in fp32 nothing is rounded to fewer bits.  A step of the fp32 instruction takes
+// four dims, or four keys: with 16 bytes per lane, element e of quarter kg is dim 16 j + 4 kg + e of step (j, e) in both operands, and the accumulator
+// of key 4 kg + e is as it stands the operand of step e of the second product.
 //
 // A wave copies a block global -> LDS (no registers, no wait) while it works on the one before.  The page numbers of a block's keys come the same way
 // one block earlier, so that the copies of a wave are the only thing its memory counter counts, and every page size goes the same way.
@@ -28,9 +30,9 @@ namespace {
 constexpr int W = 4;              // waves per workgroup
 constexpr int UNIT = 32 * W;      // keys of a unit of work: a block for every wave
 
-template <int D, int NC>
+template <typename T, int D, int NC>
 struct StreamLds {
-    static constexpr int TILE = 32 * D * 2;   // bytes of a block of 32 keys or values
+    static constexpr int TILE = 32 * D * (int)sizeof(T);   // bytes of a block of 32 keys or values
     static constexpr int C = 16 * NC;
     int32_t page[W][2][64];                   // page numbers of the keys of a wave's next blocks
     union {
@@ -41,6 +43,9 @@ struct StreamLds {
         };
     };
 };
+// Workgroups that are resident on a compute unit: as many as its LDS and registers hold.
+template <typename T, int D, int NC>
+constexpr int RESIDENT = sizeof(T) * D <= 128 ? (NC == 1 ? 4 : 3) : sizeof(T) * D <= 256 ? 2 : 1;
 
 // Units of a request: column tiles x units of keys.
 template <int C>
@@ -48,41 +53,45 @@ __device__ __forceinline__ int64_t stream_cost(const PagedArgs& a, int b, int* n
     const PagedRequest r = paged_request(a, b);
     if (req) *req = r;
     if (r.n == 0) return 0;
-    const int ct = (r.n * a.G + C - 1) / C, units = max(paged_position(a, r, r.n - 1), 0) / UNIT + 1;
+    const int ct = (int)(((int64_t)r.n * a.G + C - 1) / C), units = max(paged_position(a, r, r.n - 1), 0) / UNIT + 1;
     if (n_ct) { *n_ct = ct; *n_units = units; }
     return (int64_t)ct * units;
 }
 
-template <int D, int NC, bool ALIGNED>
+template <typename T, int D, int NC, bool ALIGNED>
 struct StreamPiece {
-    static constexpr int NJ = D / 16, NK = D / 32, VW = D / 32;   // dims per lane of a value row, matrix steps of a logit, words of a lane's values
-    static constexpr int RV = D / 8, COPIES = 32 * RV / 64;       // vectors of a row; copies of 1 KB of a block
+    static constexpr bool F32 = sizeof(T) == 4;
+    static constexpr int N = 16 / sizeof(T), NJ = D / 16;         // elements of a 16-byte vector; dims per lane of a value row
+    static constexpr int NK = D / (4 * N), VW = NJ * (int)sizeof(T) / 4;   // vectors of a lane's key (and query) row, words of its values
+    static constexpr int RV = D / N, COPIES = 32 * RV / 64;       // vectors of a row; copies of 1 KB of a block
     static constexpr int C = 16 * NC;
-    using Lds = StreamLds<D, NC>;
+    using Lds = StreamLds<T, D, NC>;
     typedef __attribute__((ext_vector_type(VW))) uint32_t VVec;
 
     // One piece: units [r0, r1) of column tile ct of request b.  whole: it is all of the item, the outputs are stored; else the partial result goes to `part`.
     static __device__ __forceinline__ void run(const PagedArgs& a, Lds& sm, const PagedRequest& rq, int b, int ct, int g, int r0, int r1, bool whole, float* part) {
         const int tid = threadIdx.x, lane = tid & 63, x = lane & 15, kg = lane >> 4;
         const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-        const int G = a.G, cols = rq.n * G, col0 = C * ct;
-        const __bf16* q_rows = (const __bf16*)a.q;
-        auto out_row = [&](int col) {   // (row, head) of a column, counted over all heads
-            const int i = paged_token(a, col);
-            return (size_t)(rq.first + i) * a.Hq + g * G + (col - i * G);
+        const int G = a.G, cols = rq.n * G, col0 = C * ct, token0 = col0 / G, head0 = col0 - token0 * G;
+        const T* q_rows = (const T*)a.q;
+        auto token_of = [&](int cl) { return token0 + paged_token(a, head0 + cl); };   // row, within the request, of column cl of the tile
+        auto out_row = [&](int cl) {   // (row, head) of a column, counted over all heads
+            const int i = paged_token(a, head0 + cl);
+            return (size_t)(rq.first + token0 + i) * a.Hq + g * G + (head0 + cl - i * G);
         };
-        bf16x8 qf[NC][NK];   // B operand of S^T = K Q^T
+        const int last_col = min(C, cols - col0) - 1;
+        u32x4 qf[NC][NK];   // B operand of S^T = K Q^T
         int pos[NC];
 #pragma unroll
         for (int nb = 0; nb < NC; ++nb) {   // columns past the end: a copy of the last
-            const int n = min(col0 + 16 * nb + x, cols - 1);
-            const __bf16* p = q_rows + out_row(n) * D + 8 * kg;
-            pos[nb] = paged_position(a, rq, paged_token(a, n));
+            const int cl = min(16 * nb + x, last_col);
+            const T* p = q_rows + out_row(cl) * D + N * kg;
+            pos[nb] = paged_position(a, rq, token_of(cl));
 #pragma unroll
-            for (int ks = 0; ks < NK; ++ks) qf[nb][ks] = *reinterpret_cast<const bf16x8*>(p + 32 * ks);
+            for (int ks = 0; ks < NK; ++ks) qf[nb][ks] = *reinterpret_cast<const u32x4*>(p + 4 * N * ks);
         }
-        const int p_first = paged_position(a, rq, paged_token(a, col0));                          // keys up to here are visible to every column
-        const int p_last = paged_position(a, rq, paged_token(a, min(col0 + C, cols) - 1));
+        const int p_first = paged_position(a, rq, token0);                     // keys up to here are visible to every column
+        const int p_last = paged_position(a, rq, token_of(last_col));
         const int n_blocks = min((p_last + 32) / 32, W * r1);                                     // (none for a tile that sees nothing)
         f32x4 o[NJ][NC];   // O^T: row m of product md is dim NJ m + md
         float m[NC], l[NC];
@@ -94,11 +103,11 @@ struct StreamPiece {
             for (int md = 0; md < NJ; ++md) o[md][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
         const int32_t* table = a.block_table + (size_t)b * a.W;
-        const uint32_t row_bytes = (uint32_t)(a.Hkv * D * 2);
-        const unsigned char *k_base = (const unsigned char*)a.k_pages + (size_t)g * D * 2, *v_base = (const unsigned char*)a.v_pages + (size_t)g * D * 2;
+        const uint32_t row_bytes = (uint32_t)(a.Hkv * D * (int)sizeof(T));
+        const unsigned char *k_base = (const unsigned char*)a.k_pages + (size_t)g * D * sizeof(T), *v_base = (const unsigned char*)a.v_pages + (size_t)g * D * sizeof(T);
         // A copy brings 64 / RV rows, RV lanes side by side to a row; copy i the rows COPIES q + i of the lanes' groups q, so that a lane's sources are
         // neighbours.  Vector c of key row r sits in place c ^ swz(r), so that the 16 rows of a fragment read meet in no bank.
-        auto swz = [](int r) { return D == 128 ? r & 15 : (r & 3) | (r >> 1 & 4); };
+        auto swz = [](int r) { return RV >= 16 ? r & 15 : (r & 3) | (r >> 1 & 4); };
         auto row_at = [](int r) { return 1024 * (r % COPIES) + 16 * RV * (r / COPIES); };
         const uint32_t k_lds = paged_lds(sm.k[wave]), v_lds = paged_lds(sm.v[wave]), page_lds = paged_lds(sm.page[wave]);
         const int qg = lane / RV, vec = lane % RV;
@@ -156,19 +165,30 @@ struct StreamPiece {
                 f32x4 s[2][NC];
                 paged_wait_but<COPIES>();   // this block's keys, and the next one's pages
                 {
-                    bf16x8 kf[2][NK];   // keys 32 blk + 16 bb + x: dims 32 ks + 8 kg ..
+                    u32x4 kf[2][NK];   // keys 32 blk + 16 bb + x: elements 4 N ks + N kg ..
 #pragma unroll
                     for (int ks = 0; ks < NK; ++ks)
 #pragma unroll
                         for (int bb = 0; bb < 2; ++bb)
-                            kf[bb][ks] = *reinterpret_cast<const bf16x8*>(sm.k[wave] + row_at(16 * bb + x) + 16 * ((4 * ks + kg) ^ swz(x)));
+                            kf[bb][ks] = *reinterpret_cast<const u32x4*>(sm.k[wave] + row_at(16 * bb + x) + 16 * ((4 * ks + kg) ^ swz(x)));
+#pragma unroll
+                    for (int bb = 0; bb < 2; ++bb)
+#pragma unroll
+                        for (int nb = 0; nb < NC; ++nb) s[bb][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int ks = 0; ks < NK; ++ks)
 #pragma unroll
-                        for (int bb = 0; bb < 2; ++bb)
+                        for (int e = 0; e < (F32 ? 4 : 1); ++e)
 #pragma unroll
-                            for (int nb = 0; nb < NC; ++nb)
-                                s[bb][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[bb][ks], qf[nb][ks], ks == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[bb][nb], 0, 0, 0);
+                            for (int bb = 0; bb < 2; ++bb)
+#pragma unroll
+                                for (int nb = 0; nb < NC; ++nb) {
+                                    if constexpr (F32)
+                                        s[bb][nb] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kf[bb][ks][e]), __uint_as_float(qf[nb][ks][e]), s[bb][nb], 0, 0, 0);
+                                    else
+                                        s[bb][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[bb][ks]), __builtin_bit_cast(bf16x8, qf[nb][ks]),
+                                                                                            s[bb][nb], 0, 0, 0);
+                                }
                 }
                 int hole_of[2] = {0, 0};   // bit v: key 16 bb + 4 kg + v of this block has no page
                 if (__builtin_expect(holes, 0)) {
@@ -213,7 +233,7 @@ struct StreamPiece {
                         for (int md = 0; md < NJ; ++md) o[md][nb] *= down;
                     }
                 }
-                u32x4 p[NC];   // weights as the B operand of the second product: slot 4 bb + v of quarter kg is key 16 bb + 4 kg + v
+                u32x4 p[NC];   // bf16: weights as the B operand of the second product: slot 4 bb + v of quarter kg is key 16 bb + 4 kg + v
 #pragma unroll
                 for (int nb = 0; nb < NC; ++nb)
 #pragma unroll
@@ -223,38 +243,51 @@ struct StreamPiece {
                             const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[bb][nb][v], a.scale_log2e, -m[nb]));
                             const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[bb][nb][v + 1], a.scale_log2e, -m[nb]));
                             l[nb] += p0 + p1;
-                            bf16x2 t;
-                            t[0] = (__bf16)p0;
-                            t[1] = (__bf16)p1;
-                            p[nb][2 * bb + v / 2] = __builtin_bit_cast(uint32_t, t);
+                            if constexpr (F32) {
+                                s[bb][nb][v] = p0;
+                                s[bb][nb][v + 1] = p1;
+                            } else {
+                                bf16x2 t;
+                                t[0] = (__bf16)p0;
+                                t[1] = (__bf16)p1;
+                                p[nb][2 * bb + v / 2] = __builtin_bit_cast(uint32_t, t);
+                            }
                         }
                 paged_wait_but<COPIES + 1>();   // this block's values
                 VVec vf[8];   // values of keys 32 blk + 16 (i / 4) + 4 kg + i % 4, dims NJ x ..
 #pragma unroll
-                for (int i = 0; i < 8; ++i) vf[i] = *reinterpret_cast<const VVec*>(sm.v[wave] + row_at(16 * (i >> 2) + 4 * kg + (i & 3)) + 2 * NJ * x);
+                for (int i = 0; i < 8; ++i) vf[i] = *reinterpret_cast<const VVec*>(sm.v[wave] + row_at(16 * (i >> 2) + 4 * kg + (i & 3)) + (int)sizeof(T) * NJ * x);
                 if (partial) {
                     bool bad = false;
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
 #pragma unroll
-                        for (int e = 0; e < VW; ++e) bad = bad || paged_not_finite(vf[i][e]);
+                        for (int e = 0; e < VW; ++e) bad = bad || paged_not_finite<T>(vf[i][e]);
                     if (__builtin_expect(__any(bad), 0)) {   // values that are not finite: not into the product
                         apart = true;
 #pragma unroll
                         for (int i = 0; i < 8; ++i)
 #pragma unroll
-                            for (int e = 0; e < VW; ++e) vf[i][e] = paged_finite_or_zero(vf[i][e]);
+                            for (int e = 0; e < VW; ++e) vf[i][e] = paged_finite_or_zero<T>(vf[i][e]);
                     }
                 }
 #pragma unroll
                 for (int md = 0; md < NJ; ++md) {
-                    u32x4 vt;   // dim NJ x + md of the eight keys
+                    if constexpr (F32) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        vt[j] = __builtin_amdgcn_perm(vf[2 * j + 1][md / 2], vf[2 * j][md / 2], md % 2 == 0 ? 0x05040100u : 0x07060302u);
+                        for (int i = 0; i < 8; ++i)
 #pragma unroll
-                    for (int nb = 0; nb < NC; ++nb)
-                        o[md][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vt), __builtin_bit_cast(bf16x8, p[nb]), o[md][nb], 0, 0, 0);
+                            for (int nb = 0; nb < NC; ++nb)
+                                o[md][nb] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vf[i][md]), s[i / 4][nb][i % 4], o[md][nb], 0, 0, 0);
+                    } else {
+                        u32x4 vt;   // dim NJ x + md of the eight keys
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            vt[j] = __builtin_amdgcn_perm(vf[2 * j + 1][md / 2], vf[2 * j][md / 2], md % 2 == 0 ? 0x05040100u : 0x07060302u);
+#pragma unroll
+                        for (int nb = 0; nb < NC; ++nb)
+                            o[md][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vt), __builtin_bit_cast(bf16x8, p[nb]), o[md][nb], 0, 0, 0);
+                    }
                 }
                 __builtin_amdgcn_sched_barrier(0);
                 asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");   // (the values have been read)
@@ -277,13 +310,13 @@ struct StreamPiece {
                         for (int i = 0; i < 32; ++i) partial = partial || !is_page(table[paged_block(a, blk0 + i)]);
                     }
                     if (!partial) continue;
-                    const uint16_t* key = (const uint16_t*)(v_base + ((size_t)page * a.P + (j - page_block * a.P)) * row_bytes);
+                    const T* key = (const T*)(v_base + ((size_t)page * a.P + (j - page_block * a.P)) * row_bytes);
 #pragma unroll
                     for (int v = 0; v < 4; ++v)
 #pragma unroll
                         for (int md = 0; md < NJ; ++md) {
-                            const uint32_t w = key[NJ * (4 * kg + v) + md];
-                            const float add = (w & 0x7F80u) == 0x7F80u ? __uint_as_float(w << 16) : 0.f;
+                            const float w = Elem<T>::to_f32(key[NJ * (4 * kg + v) + md]);
+                            const float add = (__float_as_uint(w) & 0x7F800000u) == 0x7F800000u ? w : 0.f;
 #pragma unroll
                             for (int nb = 0; nb < NC; ++nb) o[md][nb][v] += j <= pos[nb] ? add : 0.f;
                         }
@@ -305,8 +338,8 @@ struct StreamPiece {
         paged_lds_barrier();
         constexpr int NV = D / 8;
         for (int i = tid; i < C * NV; i += 64 * W) {
-            const int c = i / NV, v8 = i % NV, n = col0 + c;
-            if (n >= cols) break;
+            const int c = i / NV, v8 = i % NV;
+            if (c > last_col) break;
             float mw[W], lsum = 0.f, top = PAGED_NO_MAX;
 #pragma unroll
             for (int w = 0; w < W; ++w) { mw[w] = sm.m[c][w]; top = fmaxf(top, mw[w]); }
@@ -327,24 +360,26 @@ struct StreamPiece {
             }
             const bool none = lsum == 0.f;   // it saw nothing (the largest weight of one that did is at least 2^-8)
             const float inv_l = none ? 0.f : 1.0f / lsum;
-            struct alignas(16) { __bf16 v[8]; } y;
+            const size_t oc = out_row(c);
+            T* dst = (T*)a.out + oc * D + 8 * v8;
+            struct alignas(16) { T v[8]; } y;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                y.v[e] = (__bf16)(lo[e] * inv_l);
-                y.v[4 + e] = (__bf16)(hi[e] * inv_l);
+                y.v[e] = Elem<T>::from_f32(lo[e] * inv_l);
+                y.v[4 + e] = Elem<T>::from_f32(hi[e] * inv_l);
             }
-            const size_t oc = out_row(n);
-            *reinterpret_cast<u32x4*>((__bf16*)a.out + oc * D + 8 * v8) = __builtin_bit_cast(u32x4, y);
+#pragma unroll
+            for (int h = 0; h < (F32 ? 2 : 1); ++h) reinterpret_cast<u32x4*>(dst)[h] = reinterpret_cast<const u32x4*>(&y)[h];
             if (v8 == 0 && a.lse != nullptr) a.lse[oc] = none ? -INFINITY : (top + __builtin_amdgcn_logf(lsum)) * 0.6931471805599453f;
         }
         paged_lds_barrier();   // (the next piece's copies overwrite what was merged)
     }
 };
 
-template <int D, int NC, bool ALIGNED>
-__global__ __launch_bounds__(64 * W, 2) void paged_stream_kernel(const PagedArgs a) {
+template <typename T, int D, int NC, bool ALIGNED>
+__global__ __launch_bounds__(64 * W, (RESIDENT<T, D, NC>)) void paged_stream_kernel(const PagedArgs a) {
     extern __shared__ __attribute__((aligned(16))) unsigned char smem_raw[];
-    auto& sm = *reinterpret_cast<StreamLds<D, NC>*>(smem_raw);
+    auto& sm = *reinterpret_cast<StreamLds<T, D, NC>*>(smem_raw);
     constexpr int C = 16 * NC;
     const int g = paged_head(a), w = paged_workgroup(a);
     int64_t u = 0, end = 0;
@@ -368,7 +403,7 @@ __global__ __launch_bounds__(64 * W, 2) void paged_stream_kernel(const PagedArgs
             const int r1 = (int)min((int64_t)units, r0 + (end - u));
             const bool whole = r0 == 0 && r1 == units;
             float* part = a.partials + (((size_t)w * a.Hkv + g) * 2 + (r0 > 0 ? 0 : 1)) * (C * paged_part_floats<D>());
-            StreamPiece<D, NC, ALIGNED>::run(a, sm, rq, b, ct, g, r0, r1, whole, part);
+            StreamPiece<T, D, NC, ALIGNED>::run(a, sm, rq, b, ct, g, r0, r1, whole, part);
             u += r1 - r0;
         }
         start += cost;
@@ -377,7 +412,7 @@ __global__ __launch_bounds__(64 * W, 2) void paged_stream_kernel(const PagedArgs
 
 // Joins the pieces of the items that fell to several workgroups, in their order: blockIdx.x = (workgroup - 1) x Hkv + KV head; that workgroup's first unit, if it is the
 // first cut of an item, stands for it.  One wave per column (blockIdx.y: four of them), all of a column's pieces in one or two trips to memory.
-template <int D, int NC>
+template <typename T, int D, int NC>
 __global__ __launch_bounds__(256) void paged_stream_join_kernel(const PagedArgs a) {
     constexpr int C = 16 * NC, PF = paged_part_floats<D>(), EPT = D / 64, AHEAD = 16;
     const int g = blockIdx.x % a.Hkv, cut = blockIdx.x / a.Hkv + 1;
@@ -398,7 +433,7 @@ __global__ __launch_bounds__(256) void paged_stream_join_kernel(const PagedArgs 
     if (u == u0 || paged_owner(u0, line.total, sharers) != cut - 1) return;
     const int w0 = cut - 1, n = paged_owner(u0 + units - 1, line.total, sharers) - w0 + 1;
     const int c = 4 * blockIdx.y + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
-    if (c >= min(C, rq.n * a.G - C * ct)) return;
+    if (c >= min(C, rq.n * a.G - C * ct)) return;   // (wave-uniform)
     float top = PAGED_NO_MAX, l = 0.f, o[EPT];
 #pragma unroll
     for (int e = 0; e < EPT; ++e) o[e] = 0.f;
@@ -430,47 +465,58 @@ __global__ __launch_bounds__(256) void paged_stream_join_kernel(const PagedArgs 
             for (int e = 0; e < EPT; ++e) o[e] += po[k][e] * w;
         }
     }
-    const int col = C * ct + c, i = paged_token(a, col);
+    const int col = C * ct + c, i = col / a.G;
     const size_t oc = (size_t)(rq.first + i) * a.Hq + g * a.G + (col - i * a.G);
     const bool none = l == 0.f;
     const float inv_l = none ? 0.f : 1.0f / l;
 #pragma unroll
-    for (int e = 0; e < EPT; ++e) ((__bf16*)a.out)[oc * D + EPT * lane + e] = (__bf16)(o[e] * inv_l);
+    for (int e = 0; e < EPT; ++e) ((T*)a.out)[oc * D + EPT * lane + e] = Elem<T>::from_f32(o[e] * inv_l);
     if (lane == 0 && a.lse != nullptr) a.lse[oc] = none ? -INFINITY : (top + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
-template <int D, int NC, bool ALIGNED>
+template <typename T, int D, int NC, bool ALIGNED>
 hipError_t launch(const PagedArgs& a, int cols, hipStream_t st) {
-    using Lds = StreamLds<D, NC>;
-    static_assert(sizeof(Lds) <= 80 * 1024, "two workgroups per compute unit");
+    using Lds = StreamLds<T, D, NC>;
+    static_assert(RESIDENT<T, D, NC> * sizeof(Lds) <= 160 * 1024, "LDS of a compute unit");
     // Raises the kernel's dynamic LDS limit, once per process.
-    static const hipError_t once = hipFuncSetAttribute(reinterpret_cast<const void*>(&paged_stream_kernel<D, NC, ALIGNED>),
+    static const hipError_t once = hipFuncSetAttribute(reinterpret_cast<const void*>(&paged_stream_kernel<T, D, NC, ALIGNED>),
                                                        hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Lds));
     if (once != hipSuccess) return once;
-    paged_stream_kernel<D, NC, ALIGNED><<<dim3(paged_grid(a.n_wg, a.Hkv)), dim3(64 * W), sizeof(Lds), st>>>(a);
-    if (a.n_wg > 1) paged_stream_join_kernel<D, NC><<<dim3((unsigned)((a.n_wg - 1) * a.Hkv), (unsigned)((cols + 3) / 4)), dim3(256), 0, st>>>(a);
+    paged_stream_kernel<T, D, NC, ALIGNED><<<dim3(paged_grid(a.n_wg, a.Hkv)), dim3(64 * W), sizeof(Lds), st>>>(a);
+    if (a.n_wg > 1) paged_stream_join_kernel<T, D, NC><<<dim3((unsigned)((a.n_wg - 1) * a.Hkv), (unsigned)((cols + 3) / 4)), dim3(256), 0, st>>>(a);
     return hipGetLastError();
 }
 
-template <int D, int NC>
+template <typename T, int D, int NC>
 hipError_t launch(const PagedArgs& a, int cols, hipStream_t st) {
-    return a.P % StreamPiece<D, NC, true>::COPIES == 0 ? launch<D, NC, true>(a, cols, st) : launch<D, NC, false>(a, cols, st);
+    return a.P % StreamPiece<T, D, NC, true>::COPIES == 0 ? launch<T, D, NC, true>(a, cols, st) : launch<T, D, NC, false>(a, cols, st);
+}
+
+template <typename T, int D>
+hipError_t launch(const PagedArgs& args, int n_cu, hipStream_t st) {
+    PagedArgs a = args;
+    const int64_t most = std::min<int64_t>((int64_t)a.max_new * a.G, a.cols_hi);   // columns of a request
+    a.n_wg = std::max(1, (most <= 16 ? RESIDENT<T, D, 1> : RESIDENT<T, D, 2>) * n_cu / a.Hkv);
+    return most <= 16 ? launch<T, D, 1>(a, (int)most, st) : launch<T, D, 2>(a, (int)std::min<int64_t>(most, 32), st);
+}
+
+// Columns of all workgroups' pieces on a compute unit, the larger of the two tilings'.
+template <typename T, int D>
+constexpr int COLUMNS = std::max(16 * RESIDENT<T, D, 1>, 32 * RESIDENT<T, D, 2>);
+int columns(const Shape& s) {
+    if (s.dtype == FR_BF16) return s.d == 128 ? COLUMNS<__bf16, 128> : COLUMNS<__bf16, 64>;
+    return s.d == 128 ? COLUMNS<float, 128> : COLUMNS<float, 64>;
 }
 
 }  // namespace
 
 size_t paged_stream_partials_bytes(const Shape& s, int n_cu) {
-    return (size_t)std::max(2 * n_cu, s.Hkv) * 2 * 32 * (s.d + 2) * sizeof(float);
+    return (size_t)std::max(columns(s) * n_cu, 32 * s.Hkv) * 2 * (s.d + 2) * sizeof(float);
 }
 
-hipError_t launch_paged_stream(const Shape& s, const PagedArgs& args, int n_cu, hipStream_t st) {
-    PagedArgs a = args;
-    a.n_wg = std::max(1, 2 * n_cu / s.Hkv);   // two per compute unit are resident
-    const int64_t most = std::min<int64_t>((int64_t)a.max_new * s.G, a.cols_hi);
-    const int nc = most <= 16 ? 1 : 2;
-    const int cols = (int)std::min<int64_t>(most, 16 * nc);   // of a tile
-    if (s.d == 128) return nc == 1 ? launch<128, 1>(a, cols, st) : launch<128, 2>(a, cols, st);
-    return nc == 1 ? launch<64, 1>(a, cols, st) : launch<64, 2>(a, cols, st);
+hipError_t launch_paged_stream(const Shape& s, const PagedArgs& a, int n_cu, hipStream_t st) {
+    if (s.dtype == FR_BF16) return s.d == 128 ? launch<__bf16, 128>(a, n_cu, st) : launch<__bf16, 64>(a, n_cu, st);
+    return s.d == 128 ? launch<float, 128>(a, n_cu, st) : launch<float, 64>(a, n_cu, st);
 }
 
 }  // namespace fr

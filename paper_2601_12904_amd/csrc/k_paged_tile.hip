@@ -556,7 +556,7 @@ __device__ __forceinline__ bool process_piece(const PagedArgs& a, const PagedReq
                 u32x4 w = *reinterpret_cast<const u32x4*>(at);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const uint32_t kept = paged_finite_or_zero(w[e]);
+                    const uint32_t kept = paged_finite_or_zero<__bf16>(w[e]);
                     found = found || kept != w[e];
                     w[e] = kept;
                 }
