@@ -62,13 +62,22 @@ __device__ __forceinline__ int64_t uniform64(int64_t v) {
 
 // How a launch's work is dealt out.  The work of a KV head is one line of units: requests in order, of each its column tiles, of each its units of keys.
 // Workgroup w of n takes units floor(w U / n) .. floor((w + 1) U / n) - 1 of it, wherever they begin and end, so every workgroup has the same
-// share whatever the lengths are, and the host need not know them.  n is at most U (paged_sharers): none of them goes without.  Every item that is cut
-// is cut at the first unit of some workgroup, so a joining pass has one candidate per workgroup, however many items there are.  An item (column tile) that falls to several workgroups leaves a partial result
+// share whatever the lengths are, and the host need not know them.  n is at most U (paged_sharers): none of them goes without.  That one also
+// leaves a PagedCut, which is all that the joining pass has to read to find its work.  An item (column tile) that falls to several workgroups leaves a partial result
 // per piece: in slot 2 w of a workgroup whose piece begins behind the item's start, in 2 w + 1 of the one that has its start but not its end.
 // blockIdx.x = workgroup of the KV head x Hkv + KV head: blocks go to the eight dies in turn, so that with 8 KV heads each die's cache serves one of them.
 __device__ __forceinline__ int paged_head(const PagedArgs& a) { return blockIdx.x % a.Hkv; }
 __device__ __forceinline__ int paged_workgroup(const PagedArgs& a) { return blockIdx.x / a.Hkv; }
 inline unsigned paged_grid(int64_t workgroups, int Hkv) { return (unsigned)(workgroups * Hkv); }
+struct alignas(16) PagedCut {   // of a workgroup and KV head; in front of the partial results
+    int pieces;      // of the item that it has the start but not the end of: its own and those of the workgroups behind it; 0: there is no such item
+    int first_row;   // of the request
+    int col0, cols;  // the item's first query column, and how many the request has
+};
+__device__ __forceinline__ PagedCut* paged_cuts(const PagedArgs& a) { return reinterpret_cast<PagedCut*>(a.partials); }
+__device__ __forceinline__ float* paged_slot(const PagedArgs& a, int w, int g, int which, int floats) {
+    return a.partials + (size_t)a.n_wg * a.Hkv * (sizeof(PagedCut) / 4) + (((size_t)w * a.Hkv + g) * 2 + which) * floats;
+}
 struct PagedLine {
     int64_t total;    // U
     int64_t start;    // of the unit that was looked for: first unit of its request

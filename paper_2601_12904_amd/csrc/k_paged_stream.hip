@@ -390,9 +390,9 @@ __global__ __launch_bounds__(64 * W, (RESIDENT<T, D, NC>)) void paged_stream_ker
         end = paged_first_unit(w + 1, total, n);
         return u;
     });
-    if (line.b < 0) return;
+    PagedCut cut{0, 0, 0, 0};
     int64_t start = line.start;   // of the request's units
-    for (int b = line.b; u < end && b < a.B; ++b) {
+    for (int b = line.b; b >= 0 && u < end && b < a.B; ++b) {
         int n_ct, units;
         PagedRequest rq;
         const int64_t cost = stream_cost<C>(a, b, &n_ct, &units, &rq);
@@ -402,38 +402,27 @@ __global__ __launch_bounds__(64 * W, (RESIDENT<T, D, NC>)) void paged_stream_ker
             const int ct = (int)paged_div(in, units), r0 = (int)(in - (int64_t)ct * units);
             const int r1 = (int)min((int64_t)units, r0 + (end - u));
             const bool whole = r0 == 0 && r1 == units;
-            float* part = a.partials + (((size_t)w * a.Hkv + g) * 2 + (r0 > 0 ? 0 : 1)) * (C * paged_part_floats<D>());
+            float* part = paged_slot(a, w, g, r0 > 0 ? 0 : 1, C * paged_part_floats<D>());
+            if (r0 == 0 && r1 < units) cut = PagedCut{paged_owner(u + units - 1, line.total, paged_sharers(a, line.total)) - w + 1, rq.first, C * ct, rq.n * a.G};
             StreamPiece<T, D, NC, ALIGNED>::run(a, sm, rq, b, ct, g, r0, r1, whole, part);
             u += r1 - r0;
         }
         start += cost;
     }
+    if (threadIdx.x == 0) paged_cuts(a)[(size_t)w * a.Hkv + g] = cut;
 }
 
-// Joins the pieces of the items that fell to several workgroups, in their order: blockIdx.x = (workgroup - 1) x Hkv + KV head; that workgroup's first unit, if it is the
-// first cut of an item, stands for it.  One wave per column (blockIdx.y: four of them), all of a column's pieces in one or two trips to memory.
+// Joins the pieces of the items that fell to several workgroups, in their order: blockIdx.x = workgroup x Hkv + KV head, whose cut it sees to.  One wave per column
+// (blockIdx.y: four of them), all of a column's pieces in one or two trips to memory.
 template <typename T, int D, int NC>
 __global__ __launch_bounds__(256) void paged_stream_join_kernel(const PagedArgs a) {
     constexpr int C = 16 * NC, PF = paged_part_floats<D>(), EPT = D / 64, AHEAD = 16;
-    const int g = blockIdx.x % a.Hkv, cut = blockIdx.x / a.Hkv + 1;
-    int64_t u = 0;
-    int sharers = 0;
-    const PagedLine line = paged_line(a.B, [&](int b) { return stream_cost<C>(a, b); }, [&](int64_t total) {
-        sharers = paged_sharers(a, total);
-        if (cut >= sharers) return (int64_t)-1;
-        u = paged_first_unit(cut, total, sharers);
-        return u;
-    });
-    if (line.b < 0) return;
-    int n_ct, units;
-    PagedRequest rq;
-    stream_cost<C>(a, line.b, &n_ct, &units, &rq);
-    const int ct = (int)paged_div(u - line.start, units);
-    const int64_t u0 = line.start + (int64_t)ct * units;   // the item's first unit
-    if (u == u0 || paged_owner(u0, line.total, sharers) != cut - 1) return;
-    const int w0 = cut - 1, n = paged_owner(u0 + units - 1, line.total, sharers) - w0 + 1;
+    const int g = blockIdx.x % a.Hkv, w0 = blockIdx.x / a.Hkv;
+    const PagedCut cut = paged_cuts(a)[blockIdx.x];
+    const int n = cut.pieces;
+    if (n == 0) return;
     const int c = 4 * blockIdx.y + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
-    if (c >= min(C, rq.n * a.G - C * ct)) return;   // (wave-uniform)
+    if (c >= min(C, cut.cols - cut.col0)) return;   // (wave-uniform)
     float top = PAGED_NO_MAX, l = 0.f, o[EPT];
 #pragma unroll
     for (int e = 0; e < EPT; ++e) o[e] = 0.f;
@@ -442,7 +431,7 @@ __global__ __launch_bounds__(256) void paged_stream_join_kernel(const PagedArgs 
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) {   // (past the end: the last piece, which does not count)
             const int i = min(i0 + k, n - 1);
-            const float* p = a.partials + (((size_t)(w0 + i) * a.Hkv + g) * 2 + (i == 0 ? 1 : 0)) * (C * PF) + c * PF;
+            const float* p = paged_slot(a, w0 + i, g, i == 0 ? 1 : 0, C * PF) + c * PF;
             pm[k] = p[0];
             pl[k] = p[1];
 #pragma unroll
@@ -465,8 +454,8 @@ __global__ __launch_bounds__(256) void paged_stream_join_kernel(const PagedArgs 
             for (int e = 0; e < EPT; ++e) o[e] += po[k][e] * w;
         }
     }
-    const int col = C * ct + c, i = col / a.G;
-    const size_t oc = (size_t)(rq.first + i) * a.Hq + g * a.G + (col - i * a.G);
+    const int col = cut.col0 + c, i = col / a.G;
+    const size_t oc = (size_t)(cut.first_row + i) * a.Hq + g * a.G + (col - i * a.G);
     const bool none = l == 0.f;
     const float inv_l = none ? 0.f : 1.0f / l;
 #pragma unroll
@@ -511,7 +500,7 @@ int columns(const Shape& s) {
 }  // namespace
 
 size_t paged_stream_partials_bytes(const Shape& s, int n_cu) {
-    return (size_t)std::max(columns(s) * n_cu, 32 * s.Hkv) * 2 * (s.d + 2) * sizeof(float);
+    return (size_t)std::max(columns(s) * n_cu, 32 * s.Hkv) * 2 * (s.d + 2) * sizeof(float) + (size_t)std::max(4 * n_cu, s.Hkv) * sizeof(PagedCut);
 }
 
 hipError_t launch_paged_stream(const Shape& s, const PagedArgs& a, int n_cu, hipStream_t st) {

@@ -770,10 +770,10 @@ __global__ __launch_bounds__(64 * WAVES) void paged_tile_kernel(const PagedArgs 
     extern __shared__ __attribute__((aligned(16))) unsigned char smem_raw[];
     const int g = paged_head(a), w = paged_workgroup(a);
     const TilePlan plan = tile_plan(a, w, w);
-    if (plan.b < 0) return;
+    PagedCut cut{0, 0, 0, 0};
     int64_t u = plan.whole ? 0 : paged_first_unit(w, plan.total, plan.sharers), start = plan.start;
     const int64_t end = plan.whole ? 0 : paged_first_unit(w + 1, plan.total, plan.sharers);
-    for (int b = plan.b; b < a.B;) {
+    for (int b = plan.b; b >= 0 && b < a.B;) {
         const PagedRequest rq = paged_request(a, b);
         const TileCosts c = tile_costs(a, rq);
         const int64_t all = rq.n > 0 ? c.before(c.n_ct) : 0;
@@ -787,34 +787,28 @@ __global__ __launch_bounds__(64 * WAVES) void paged_tile_kernel(const PagedArgs 
         const int n = (paged_position(a, rq, i) + KT) / KT;                                              // its key tiles
         const int64_t cost = c.tile(t), x0 = plan.whole ? 0 : u - start - c.before(t), x1 = plan.whole ? cost : min(cost, x0 + (end - u));
         const int kb = x0 == 0 ? 0 : (int)paged_div(x0 * n, cost), ke = x1 == cost ? n : (int)paged_div(x1 * n, cost);
-        float* part = a.partials + (((size_t)w * a.Hkv + g) * 2 + (x0 > 0 ? 0 : 1)) * (C * paged_part_floats<D>());
+        float* part = paged_slot(a, w, g, x0 > 0 ? 0 : 1, C * paged_part_floats<D>());
+        if (x0 == 0 && x1 < cost) cut = PagedCut{paged_owner(u + cost - 1, plan.total, plan.sharers) - w + 1, rq.first, C * t, rq.n * a.G};
         const bool whole = x0 == 0 && x1 == cost;
         if (!process_piece<D, ALIGNED, false>(a, rq, b, t, g, kb, ke, whole, part, smem_raw))
             process_piece<D, ALIGNED, true>(a, rq, b, t, g, kb, ke, whole, part, smem_raw);
         u += x1 - x0;
-        if (plan.whole || u >= end) return;
+        if (plan.whole || u >= end) break;
     }
+    if (threadIdx.x == 0 && w < a.n_wg) paged_cuts(a)[(size_t)w * a.Hkv + g] = cut;
 }
 
-// Joins the pieces of the items that fell to several workgroups, in their order: blockIdx.x = (workgroup - 1) x Hkv + KV head; that workgroup's first unit, if it is the
-// first cut of an item, stands for it.  blockIdx.y: 16 columns, 16 threads each.
+// Joins the pieces of the items that fell to several workgroups, in their order: blockIdx.x = workgroup x Hkv + KV head, whose cut it sees to.  blockIdx.y: 16 columns,
+// 16 threads each.
 template <int D>
 __global__ __launch_bounds__(256) void paged_tile_join_kernel(const PagedArgs a) {
-    const int g = blockIdx.x % a.Hkv, cut = blockIdx.x / a.Hkv + 1;
-    const TilePlan plan = tile_plan(a, 0, cut);
-    if (plan.whole || plan.b < 0) return;
-    const PagedRequest rq = paged_request(a, plan.b);
-    const TileCosts c = tile_costs(a, rq);
-    const int64_t u = paged_first_unit(cut, plan.total, plan.sharers);
-    const int t = c.tile_at(u - plan.start);
-    const int64_t u0 = plan.start + c.before(t);   // the item's first unit
-    if (u == u0 || paged_owner(u0, plan.total, plan.sharers) != cut - 1) return;
-    const int w0 = cut - 1, n = paged_owner(u0 + c.tile(t) - 1, plan.total, plan.sharers) - w0 + 1;
+    const int g = blockIdx.x % a.Hkv, w0 = blockIdx.x / a.Hkv;
+    const PagedCut cut = paged_cuts(a)[blockIdx.x];
+    const int n = cut.pieces;
+    if (n == 0) return;
     constexpr int NV = D / 64, AHEAD = 8;   // vectors of a thread; pieces in flight
     const int cl = 16 * blockIdx.y + threadIdx.x / 16, e0 = 4 * (threadIdx.x % 16);
-    TileItem<D> it;
-    it.init(a, rq, t, g);
-    if (it.col0 + cl >= it.cols) return;
+    if (cut.col0 + cl >= cut.cols) return;
     float top = PAGED_NO_MAX, l = 0.f;
     f32x4 o[NV];
 #pragma unroll
@@ -825,7 +819,7 @@ __global__ __launch_bounds__(256) void paged_tile_join_kernel(const PagedArgs a)
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) {   // (past the end: the last piece, which does not count)
             const int i = min(i0 + k, n - 1);
-            const float* part = a.partials + (((size_t)(w0 + i) * a.Hkv + g) * 2 + (i == 0 ? 1 : 0)) * (C * paged_part_floats<D>());
+            const float* part = paged_slot(a, w0 + i, g, i == 0 ? 1 : 0, C * paged_part_floats<D>());
             pm[k] = part[2 * cl];
             pl[k] = part[2 * cl + 1];
 #pragma unroll
@@ -843,7 +837,8 @@ __global__ __launch_bounds__(256) void paged_tile_join_kernel(const PagedArgs a)
     }
     const bool none = l == 0.f;
     const float inv_l = none ? 0.f : 1.0f / l;
-    const size_t oc = it.out_row(a, cl);
+    const int col = cut.col0 + cl, i = col / a.G;
+    const size_t oc = (size_t)(cut.first_row + i) * a.Hq + g * a.G + (col - i * a.G);
     typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
@@ -876,7 +871,7 @@ int tile_workgroups(int Hkv, int n_cu) { return std::max(1, n_cu / Hkv); }   // 
 }  // namespace
 
 size_t paged_tile_partials_bytes(const Shape& s, int n_cu) {
-    return (size_t)tile_workgroups(s.Hkv, n_cu) * s.Hkv * 2 * C * (s.d + 2) * sizeof(float);
+    return (size_t)tile_workgroups(s.Hkv, n_cu) * s.Hkv * (2 * C * (s.d + 2) * sizeof(float) + sizeof(PagedCut));
 }
 
 hipError_t launch_paged_tile(const Shape& s, const PagedArgs& args, int n_cu, hipStream_t st) {
