@@ -472,7 +472,8 @@ hipError_t launch(const PagedArgs& a, int cols, hipStream_t st) {
                                                        hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Lds));
     if (once != hipSuccess) return once;
     paged_stream_kernel<T, D, NC, ALIGNED><<<dim3(paged_grid(a.n_wg, a.Hkv)), dim3(64 * W), sizeof(Lds), st>>>(a);
-    if (a.n_wg > 1) paged_stream_join_kernel<T, D, NC><<<dim3((unsigned)((a.n_wg - 1) * a.Hkv), (unsigned)((cols + 3) / 4)), dim3(256), 0, st>>>(a);
+    if (a.n_wg > 1 && a.cap > UNIT)   // (else every item is one unit, and none is cut)
+        paged_stream_join_kernel<T, D, NC><<<dim3((unsigned)((a.n_wg - 1) * a.Hkv), (unsigned)((cols + 3) / 4)), dim3(256), 0, st>>>(a);
     return hipGetLastError();
 }
 
@@ -500,7 +501,8 @@ int columns(const Shape& s) {
 }  // namespace
 
 size_t paged_stream_partials_bytes(const Shape& s, int n_cu) {
-    return (size_t)std::max(columns(s) * n_cu, 32 * s.Hkv) * 2 * (s.d + 2) * sizeof(float) + (size_t)std::max(4 * n_cu, s.Hkv) * sizeof(PagedCut);
+    // (one workgroup per KV head, where there are more of those than workgroups: nothing is cut)
+    return (size_t)columns(s) * n_cu * 2 * (s.d + 2) * sizeof(float) + (size_t)std::max(4 * n_cu, s.Hkv) * sizeof(PagedCut);
 }
 
 hipError_t launch_paged_stream(const Shape& s, const PagedArgs& a, int n_cu, hipStream_t st) {

@@ -871,7 +871,8 @@ int tile_workgroups(int Hkv, int n_cu) { return std::max(1, n_cu / Hkv); }   // 
 }  // namespace
 
 size_t paged_tile_partials_bytes(const Shape& s, int n_cu) {
-    return (size_t)tile_workgroups(s.Hkv, n_cu) * s.Hkv * (2 * C * (s.d + 2) * sizeof(float) + sizeof(PagedCut));
+    const int n = tile_workgroups(s.Hkv, n_cu);   // (one: nothing is cut)
+    return (size_t)n * s.Hkv * ((n > 1 ? 2 * C * (s.d + 2) * sizeof(float) : 0) + sizeof(PagedCut));
 }
 
 hipError_t launch_paged_tile(const Shape& s, const PagedArgs& args, int n_cu, hipStream_t st) {
