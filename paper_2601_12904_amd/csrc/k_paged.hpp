@@ -6,6 +6,8 @@
 namespace fr {
 
 // Arguments of the kernels.  A launch takes the requests with cols_lo < rows x G <= cols_hi query columns.
+// route: whether requests with more than `few` columns go through the tiled kernel is for the kernels to find out (paged_route); if they do, those with fewer go with
+// them where `together` says so.
 struct PagedArgs {
     const void* q;
     const int32_t *q_offsets, *cached_len, *block_table;
@@ -15,6 +17,7 @@ struct PagedArgs {
     float* partials;
     int B, T, max_new, n_pages, P, W, cap;   // cap = W P: positions that the table has room for
     int Hq, Hkv, G, cols_lo, cols_hi;
+    int route, few, together;
     int n_wg;                // workgroups per KV head that the work is dealt to
     uint32_t g_magic;        // ceil(2^32 / G): c / G = mulhi(c, g_magic) for c < 2^26
     uint32_t p_magic, p_shift;   // j / P = mulhi(2 j, p_magic) >> p_shift for j < 2^30
@@ -69,6 +72,32 @@ __device__ __forceinline__ int64_t uniform64(int64_t v) {
 __device__ __forceinline__ int paged_head(const PagedArgs& a) { return blockIdx.x % a.Hkv; }
 __device__ __forceinline__ int paged_workgroup(const PagedArgs& a) { return blockIdx.x / a.Hkv; }
 inline unsigned paged_grid(int64_t workgroups, int Hkv) { return (unsigned)(workgroups * Hkv); }
+// Do the requests with many columns go through the tiled kernel?  It takes 45 us for the first key tile of every request and 1.5 us for 256 columns x 64 keys on a
+// compute unit, the streaming kernel 11 us and twice the time per column, and it reads the keys again for every 32 columns, from the die's cache as
+// long as they fit about twice.  us tiled : streaming, rows behind positions (columns x keys of all KV heads); 32 / 8 heads: 128 behind 1000 (5 M) 58 : 23, 512 behind 4000 (74 M) 103 : 68,
+// 512 behind 14336 (243 M) 167 : 196, 1024 from nothing (34 M) 63 : 42, 2048 (134 M) 90 : 112; 64 / 8 heads: 512 behind 4000 (148 M) 128 : 126, 128 behind 14336 (118 M) 98 : 110;
+// sixteen times 40 behind 3000: 32 / 8 heads (62 M, 25 MB per KV head) 107 : 168, head_dim 64 (31 M, 12 MB) 59 : 41.
+constexpr int64_t PAGED_PAIRS_NEAR = 100000000, PAGED_PAIRS_FAR = 35000000;   // columns x keys; the keys of a KV head in PAGED_NEAR_BYTES, or more
+constexpr int64_t PAGED_NEAR_BYTES = 8 << 20;
+__device__ __forceinline__ bool paged_route(const PagedArgs& a, int row_bytes) {
+    const int lane = threadIdx.x & 63;
+    int64_t pairs = 0, keys = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 64) {
+        int64_t p = 0, k = 0;
+        if (b0 + lane < a.B) {
+            const int b = b0 + lane, lo = max(min(a.q_offsets[b], a.T), 0), hi = max(min(a.q_offsets[b + 1], a.T), lo);
+            const int64_t cols = (int64_t)min(hi - lo, a.max_new) * a.G;
+            if (cols > a.few) {
+                k = max((int64_t)0, min((int64_t)a.cached_len[b] + (hi - lo), (int64_t)a.cap));
+                p = cols * k >> 10;   // (in thousands: no sum passes 64 bits)
+            }
+        }
+        pairs += uniform64(wave_sum64(p, min(64, a.B - b0)));
+        keys += uniform64(wave_sum64(k, min(64, a.B - b0)));
+    }
+    return pairs * a.Hkv > (keys * row_bytes <= PAGED_NEAR_BYTES ? PAGED_PAIRS_NEAR : PAGED_PAIRS_FAR) >> 10;
+}
+
 struct alignas(16) PagedCut {   // of a workgroup and KV head; in front of the partial results
     int pieces;      // of the item that it has the start but not the end of: its own and those of the workgroups behind it; 0: there is no such item
     int first_row;   // of the request

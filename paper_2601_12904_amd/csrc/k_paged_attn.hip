@@ -5,7 +5,8 @@
 //
 // Which kernels a call takes.  The lengths are on the device; the host knows the number of requests and rows and a bound on the rows of one.  A request with few query columns
 // (rows x heads of a group) is bound by the bytes of its keys and values: k_paged_stream.hip; one with many by the matrix instructions: k_paged_tile.hip, whose
-// tile of 256 columns takes 1.5 us per 64 keys however few of them there are.
+// tile of 256 columns takes 1.5 us per 64 keys however few of them there are.  Where the total decides and the host's bounds do not (a table has room for more than
+// its requests hold), both are launched and find out which of them works (paged_route); the other one's launch and its joining pass take 9 us.
 #include "k_paged.hpp"
 
 #include <algorithm>
@@ -33,16 +34,21 @@ hipError_t launch_paged_attn(const Shape& s, const PagedAttnArgs& args, float* p
     // apart : together, one request of 777 rows behind 4000 and n of one row behind 2000 - 8000; 32 / 8 heads n = 4 150 : 138, 8 153 : 145, 16 202 : 193, 32 269 : 303, 63 373 : 532;
     // 28 / 4 heads n = 8 142 : 125, 16 154 : 143, 32 200 : 206; 16 / 8 heads, head_dim 64, n = 4 71 : 65, 8 80 : 80, 16 92 : 103; behind 100 - 1000 rows
     // of 32 / 8 heads n = 4 138 : 126, 8 135 : 144, 16 144 : 155.
-    const int few = std::max(64, s.G);
-    const bool others = (int64_t)args.max_new * s.G > few;
-    a.cols_lo = 0;
-    a.cols_hi = few;
-    if (!others || (int64_t)(args.n_requests - 1) * s.Hkv > n_cu / 4) {
-        hipError_t e = launch_paged_stream(s, a, n_cu, st);
-        if (e != hipSuccess || !others) return e;
-        a.cols_lo = few;
-    }
+    a.few = std::max(64, s.G);
     a.cols_hi = INT32_MAX;
+    const int64_t rows = std::min<int64_t>(a.T, (int64_t)a.B * a.max_new);
+    // columns x keys of all KV heads (paged_route): no more than what the table has room for, no less than the chunks themselves
+    const double most = (double)rows * s.Hq * a.cap, least = (double)rows * rows / a.B * s.Hq;
+    if ((int64_t)args.max_new * s.G <= a.few || most <= (double)PAGED_PAIRS_FAR) return launch_paged_stream(s, a, n_cu, st);
+    a.together = (int64_t)(args.n_requests - 1) * s.Hkv <= n_cu / 4;
+    a.route = least <= (double)PAGED_PAIRS_NEAR;
+    if (a.route || !a.together) {
+        if (!a.route) a.cols_hi = a.few;
+        hipError_t e = launch_paged_stream(s, a, n_cu, st);
+        if (e != hipSuccess) return e;
+        a.cols_hi = INT32_MAX;
+    }
+    a.cols_lo = a.together ? 0 : a.few;
     return launch_paged_tile(s, a, n_cu, st);
 }
 

@@ -377,8 +377,13 @@ struct StreamPiece {
 };
 
 template <typename T, int D, int NC, bool ALIGNED>
-__global__ __launch_bounds__(64 * W, (RESIDENT<T, D, NC>)) void paged_stream_kernel(const PagedArgs a) {
+__global__ __launch_bounds__(64 * W, (RESIDENT<T, D, NC>)) void paged_stream_kernel(const PagedArgs args) {
     extern __shared__ __attribute__((aligned(16))) unsigned char smem_raw[];
+    PagedArgs a = args;
+    if (a.route) {   // all requests, those with few columns, or none
+        a.cols_lo = 0;
+        a.cols_hi = !paged_route(a, D * (int)sizeof(T) * 2) ? INT32_MAX : a.together ? 0 : a.few;
+    }
     auto& sm = *reinterpret_cast<StreamLds<T, D, NC>*>(smem_raw);
     constexpr int C = 16 * NC;
     const int g = paged_head(a), w = paged_workgroup(a);

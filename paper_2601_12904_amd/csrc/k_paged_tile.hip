@@ -766,8 +766,13 @@ __device__ __forceinline__ bool process_piece(const PagedArgs& a, const PagedReq
 }
 
 template <int D, bool ALIGNED>
-__global__ __launch_bounds__(64 * WAVES) void paged_tile_kernel(const PagedArgs a) {
+__global__ __launch_bounds__(64 * WAVES) void paged_tile_kernel(const PagedArgs args) {
     extern __shared__ __attribute__((aligned(16))) unsigned char smem_raw[];
+    PagedArgs a = args;
+    if (a.route) {   // the requests with many columns, all, or none
+        a.cols_hi = INT32_MAX;
+        a.cols_lo = !paged_route(a, D * 4) ? INT32_MAX : a.together ? 0 : a.few;
+    }
     const int g = paged_head(a), w = paged_workgroup(a);
     const TilePlan plan = tile_plan(a, w, w);
     PagedCut cut{0, 0, 0, 0};
@@ -859,7 +864,7 @@ hipError_t launch(const PagedArgs& a, hipStream_t st) {
     if (once != hipSuccess) return once;
     // no more items than this: full tiles of all rows, and one that is not full per request
     const int64_t rows = std::min<int64_t>(a.T, (int64_t)a.B * a.max_new);
-    const int64_t items = rows * a.G / C + std::min<int64_t>(a.B, rows * a.G / (a.cols_lo + 1));
+    const int64_t items = rows * a.G / C + std::min<int64_t>(a.B, rows * a.G / ((int64_t)a.cols_lo + 1));
     const int64_t grid = std::max<int64_t>(a.n_wg, items);
     paged_tile_kernel<D, ALIGNED><<<dim3(paged_grid(grid, a.Hkv)), dim3(64 * WAVES), tile_lds_bytes<D>(), st>>>(a);
     if (a.n_wg > 1) paged_tile_join_kernel<D><<<dim3((unsigned)((a.n_wg - 1) * a.Hkv), C / 16), dim3(256), 0, st>>>(a);
