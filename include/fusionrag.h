@@ -112,13 +112,16 @@ int64_t fr_workspace_bytes(const fr_ctx* ctx);
  * workgroups (one per CU), the tiles of that round are split along K over several workgroups each and a second small
  * kernel adds the parts; 0: never.  Same results up to fp32 summation order; for tests and tuning.  (Like every
  * option these two belong to the context they are set on.)
+ * FR_OPT_PAGED_KERNEL: AUTO (default) lets fr_paged_attn choose, by the rows and positions of a bf16 call's requests, between the kernel that
+ * streams the pages and the one that tiles them; STREAM and TILED force one of them (fp32 contexts always stream), so that tests reach both.
  * FR_OPT_ATTN_KERNEL_TIMER: value n in [0, 256]: the bf16 attention launch attaches an event pair to the dispatch of
  * its dominant kernel (the key-tile loop; a short prompt's only one) on the call's stream, start and end of that kernel's execution, and keeps
  * the last n pairs; 0 (default) switches the timer off.  Read with fr_attn_kernel_times.  For benchmarks: the events
  * see one kernel, not the whole call. */
 typedef enum { FR_OPT_ATTN_SOFTMAX = 1, FR_OPT_ATTN_SPLIT = 2, FR_OPT_DECODE_KERNEL = 3, FR_OPT_GEMM_TILE = 4,
-               FR_OPT_ATTN_KERNEL_TIMER = 5, FR_OPT_GEMM_TAIL_SPLIT = 6 } fr_option;
+               FR_OPT_ATTN_KERNEL_TIMER = 5, FR_OPT_GEMM_TAIL_SPLIT = 6, FR_OPT_PAGED_KERNEL = 7 } fr_option;
 typedef enum { FR_DECODE_KERNEL_AUTO = 0, FR_DECODE_KERNEL_GENERIC = 1 } fr_decode_kernel;
+typedef enum { FR_PAGED_KERNEL_AUTO = 0, FR_PAGED_KERNEL_STREAM = 1, FR_PAGED_KERNEL_TILED = 2 } fr_paged_kernel;
 typedef enum { FR_ATTN_SOFTMAX_AUTO = 0, FR_ATTN_SOFTMAX_RUNNING_MAX = 1 } fr_attn_softmax;
 typedef enum { FR_ATTN_SPLIT_AUTO = 0, FR_ATTN_SPLIT_OFF = 1, FR_ATTN_SPLIT_ON = 2 } fr_attn_split;
 fr_status fr_set_option(fr_ctx* ctx, int32_t option, int64_t value);
@@ -332,7 +335,7 @@ fr_status fr_mark_stale_rows(fr_ctx* ctx, uint32_t* stale_bits, int64_t n_words,
  *                     and is that request's position cached_len[b] + t - q_offsets[b].  Ascending
  * A step is fr_page_tables, then per layer fr_paged_append and fr_paged_attn; the lengths stay on the device, so a captured
  * step is replayed for other lengths.  The context's max_tokens bounds none of this; max_blocks * page_rows and n_tokens
- * are at most 2^30, n_pages * page_rows at most 2^31 - 1 (FR_ERR_UNSUPPORTED beyond). */
+ * are at most 2^30, n_pages * page_rows and, in fr_paged_attn, n_tokens * n_q_heads at most 2^31 - 1 (FR_ERR_UNSUPPORTED beyond). */
 #define FR_PAGED_MAX_REQUESTS 4096
 
 /* Tables of a step from the requests' lengths.  Request b brings new_len[b] rows: they are rows q_offsets[b] ..

@@ -27,7 +27,9 @@ FR_OPT_DECODE_KERNEL = 3
 FR_OPT_GEMM_TILE = 4
 FR_OPT_GEMM_TAIL_SPLIT = 6
 FR_OPT_ATTN_KERNEL_TIMER = 5
+FR_OPT_PAGED_KERNEL = 7
 FR_DECODE_KERNEL_AUTO, FR_DECODE_KERNEL_GENERIC = 0, 1
+FR_PAGED_KERNEL_AUTO, FR_PAGED_KERNEL_STREAM, FR_PAGED_KERNEL_TILED = 0, 1, 2
 FR_ATTN_SOFTMAX_AUTO, FR_ATTN_SOFTMAX_RUNNING_MAX = 0, 1
 FR_ATTN_SPLIT_AUTO, FR_ATTN_SPLIT_OFF, FR_ATTN_SPLIT_ON = 0, 1, 2
 EXPORTS = ("fr_create", "fr_destroy", "fr_last_error", "fr_workspace_bytes", "fr_set_option", "fr_attn_kernel_times", "fr_topk_count", "fr_rope_shift",

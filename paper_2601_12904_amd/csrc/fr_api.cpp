@@ -228,6 +228,11 @@ fr_status fr_set_option(fr_ctx* ctx, int32_t option, int64_t value) {
                 return fail(ctx, FR_ERR_INVALID_ARG, "FR_OPT_DECODE_KERNEL: unknown value %lld", (long long)value);
             ctx->decode_generic = (value == FR_DECODE_KERNEL_GENERIC) ? 1 : 0;
             return FR_OK;
+        case FR_OPT_PAGED_KERNEL:
+            if (value != FR_PAGED_KERNEL_AUTO && value != FR_PAGED_KERNEL_STREAM && value != FR_PAGED_KERNEL_TILED)
+                return fail(ctx, FR_ERR_INVALID_ARG, "FR_OPT_PAGED_KERNEL: unknown value %lld", (long long)value);
+            ctx->paged_kernel = (int)value;
+            return FR_OK;
         case FR_OPT_ATTN_KERNEL_TIMER: {
             if (value < 0 || value > KernelTimer::MAX_SLOTS)
                 return fail(ctx, FR_ERR_INVALID_ARG, "FR_OPT_ATTN_KERNEL_TIMER: %lld slots outside [0, %d]", (long long)value,
@@ -934,7 +939,7 @@ fr_status fr_paged_attn(fr_ctx* ctx, const void* q, const int32_t* q_offsets, co
     a.q = q; a.q_offsets = q_offsets; a.cached_len = cached_len; a.n_requests = n_requests; a.n_tokens = n_tokens;
     a.max_new = max_new < n_tokens ? max_new : n_tokens;
     a.k_pages = k_pages; a.v_pages = v_pages; a.n_pages = n_pages; a.page_rows = page_rows;
-    a.block_table = block_table; a.max_blocks = max_blocks; a.out = out; a.lse = lse_out;
+    a.block_table = block_table; a.max_blocks = max_blocks; a.out = out; a.lse = lse_out; a.kernel = ctx->paged_kernel;
     hipError_t e = launch_paged_attn(ctx->shape, a, ctx->ws.decode_partials, ctx->ws.n_cu, (hipStream_t)stream);
     if (e != hipSuccess) return hip_fail(ctx, "paged attention launch", e);
     return FR_OK;

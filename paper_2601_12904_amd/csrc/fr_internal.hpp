@@ -94,6 +94,7 @@ struct fr_ctx {
     int attn_softmax_mode = FR_ATTN_SOFTMAX_AUTO;
     int attn_split_mode = FR_ATTN_SPLIT_AUTO;
     int decode_generic = 0;
+    int paged_kernel = FR_PAGED_KERNEL_AUTO;
     fr::GemmTuning gemm_tuning;
     fr::KernelTimer attn_timer;
     std::string err;
@@ -201,6 +202,7 @@ struct PagedAttnArgs {
     const void *k_pages, *v_pages; int n_pages, page_rows;
     const int32_t* block_table; int max_blocks;
     void* out; float* lse;
+    int kernel;   // FR_PAGED_KERNEL_*
 };
 size_t paged_attn_partials_bytes(const Shape& s, int n_cu);
 hipError_t launch_paged_attn(const Shape& s, const PagedAttnArgs& a, float* partials, int n_cu, hipStream_t st);

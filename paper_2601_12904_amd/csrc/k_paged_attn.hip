@@ -26,7 +26,7 @@ hipError_t launch_paged_attn(const Shape& s, const PagedAttnArgs& args, float* p
     while (((int64_t)1 << a.p_shift) < a.P) ++a.p_shift;
     a.p_magic = (uint32_t)(2 * ((((uint64_t)1 << (30 + a.p_shift)) + a.P - 1) / a.P));
     a.scale_log2e = (1.0f / sqrtf((float)s.d)) * 1.4426950408889634f;
-    if (s.dtype != FR_BF16) {
+    if (s.dtype != FR_BF16 || args.kernel == FR_PAGED_KERNEL_STREAM) {
         a.cols_hi = INT32_MAX;
         return launch_paged_stream(s, a, n_cu, st);
     }
@@ -36,6 +36,7 @@ hipError_t launch_paged_attn(const Shape& s, const PagedAttnArgs& args, float* p
     // of 32 / 8 heads n = 4 138 : 126, 8 135 : 144, 16 144 : 155.
     a.few = std::max(64, s.G);
     a.cols_hi = INT32_MAX;
+    if (args.kernel == FR_PAGED_KERNEL_TILED) return launch_paged_tile(s, a, n_cu, st);
     const int64_t rows = std::min<int64_t>(a.T, (int64_t)a.B * a.max_new);
     // columns x keys of all KV heads (paged_route): no more than what the table has room for, no less than the chunks themselves
     const double most = (double)rows * s.Hq * a.cap, least = (double)rows * rows / a.B * s.Hq;

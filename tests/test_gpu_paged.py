@@ -24,10 +24,12 @@ LAYERS = {
 }
 
 
-def make_ctx(layer, half=False, base=5e5, tokens=64):
+def make_ctx(layer, half=False, base=5e5, tokens=64, kernel="auto"):
     Hq, Hkv, d, dt = layer
-    return B.Context(Hq, Hkv, d, B.FR_BF16 if dt == "bf16" else B.FR_F32, base, max_tokens=tokens, max_chunks=1, max_question_tokens=1,
-                     rope_layout=B.FR_ROPE_HALF if half else B.FR_ROPE_INTERLEAVED)
+    c = B.Context(Hq, Hkv, d, B.FR_BF16 if dt == "bf16" else B.FR_F32, base, max_tokens=tokens, max_chunks=1, max_question_tokens=1,
+                  rope_layout=B.FR_ROPE_HALF if half else B.FR_ROPE_INTERLEAVED)
+    c.fr_set_option(B.FR_OPT_PAGED_KERNEL, {"auto": B.FR_PAGED_KERNEL_AUTO, "stream": B.FR_PAGED_KERNEL_STREAM, "tiled": B.FR_PAGED_KERNEL_TILED}[kernel])
+    return c
 
 
 def i32(v):
@@ -186,15 +188,17 @@ FORMS = {
     "prompt": [(0, 300)],
     "mixed": [(90, 1), (200, 130), (0, 1), (3, 0), (1000, 2), (0, 0), (64, 64)],
     "long_chunk": [(1500, 200)],
+    "few_behind_many": [(6000, 70)],      # (the tiled kernel cuts it)
 }
+BOTH = [(k, l) for k in ("auto", "tiled") for l in LAYERS if k == "auto" or LAYERS[l][3] == "bf16"]
 
 
-@pytest.mark.parametrize("layer", list(LAYERS))
+@pytest.mark.parametrize("kernel,layer", BOTH)
 @pytest.mark.parametrize("form", list(FORMS))
-def test_attention(layer, form):
-    page = {"decode": 16, "one_long": 16, "verify": 8, "chunk": 64, "prompt": 32, "mixed": 24, "long_chunk": 128}[form]
+def test_attention(kernel, layer, form):
+    page = {"decode": 16, "one_long": 16, "verify": 8, "chunk": 64, "prompt": 32, "mixed": 24, "long_chunk": 128, "few_behind_many": 16}[form]
     bt = make_batch(LAYERS[layer], FORMS[form], page, seed=len(layer) + len(form))
-    ctx = make_ctx(LAYERS[layer])
+    ctx = make_ctx(LAYERS[layer], kernel=kernel)
     out, lse = run_attn(ctx, bt)
     rows = None if len(bt["q"]) < 60 else {int(t) for o in bt["offs"] for t in (o - 2, o - 1, o, o + 1)} | set(range(0, len(bt["q"]), 13))
     check_attn(bt, out, lse, rows)
@@ -203,11 +207,14 @@ def test_attention(layer, form):
     ctx.close()
 
 
-@pytest.mark.parametrize("layer", ["g4", "g2_d64", "f32_d64"])
-@pytest.mark.parametrize("form", ["decode", "one_long", "verify", "mixed", "long_chunk"])
-def test_what_an_earlier_call_left_in_the_workspace(layer, form):
+FEW = [("auto", "g4"), ("auto", "g2_d64"), ("auto", "f32_d64"), ("tiled", "g4"), ("tiled", "g2_d64")]
+
+
+@pytest.mark.parametrize("kernel,layer", FEW)
+@pytest.mark.parametrize("form", ["decode", "one_long", "verify", "mixed", "long_chunk", "few_behind_many"])
+def test_what_an_earlier_call_left_in_the_workspace(kernel, layer, form):
     """Partial results of a batch that is NaN throughout lie where the next call's go: nothing of them is read."""
-    ctx = make_ctx(LAYERS[layer])
+    ctx = make_ctx(LAYERS[layer], kernel=kernel)
     for lens in ([(900, 1)] * 40, [(1000, 300), (500, 200)], [(6000, 1)], [(3000, 70)]):
         nan = make_batch(LAYERS[layer], lens, 16, seed=1)
         nan["kp"][:], nan["vp"][:] = np.nan, np.nan
@@ -219,17 +226,17 @@ def test_what_an_earlier_call_left_in_the_workspace(layer, form):
 
 
 @pytest.mark.parametrize("page", [1, 2, 3, 5, 8, 12, 16, 20, 31, 100, 256, 5000])
-@pytest.mark.parametrize("layer", ["g4", "g2_d64", "f32_d64"])
-def test_page_sizes(layer, page):
+@pytest.mark.parametrize("kernel,layer", FEW)
+def test_page_sizes(kernel, layer, page):
     bt = make_batch(LAYERS[layer], [(333, 1), (64, 70), (0, 3)], page, seed=page)
-    ctx = make_ctx(LAYERS[layer])
+    ctx = make_ctx(LAYERS[layer], kernel=kernel)
     out, lse = run_attn(ctx, bt)
     check_attn(bt, out, lse, set(range(0, 74, 5)) | {0, 1, 70, 71, 73})
     ctx.close()
 
 
-@pytest.mark.parametrize("layer", ["g4", "g7", "g8_d64", "f32_g5_d128"])
-def test_what_a_row_does_not_see(layer):
+@pytest.mark.parametrize("kernel,layer", [(k, l) for k in ("auto", "tiled") for l in ("g4", "g7", "g8_d64", "f32_g5_d128") if (k, l) != ("tiled", "f32_g5_d128")])
+def test_what_a_row_does_not_see(kernel, layer):
     """Values and keys of later rows of the chunk that are not finite, pages that are not there, rows that see nothing."""
     bt = make_batch(LAYERS[layer], [(100, 40), (37, 1), (-3, 6), (-9, 4), (200, 90)], 16, seed=5, pad=4)
     Hq, Hkv, d, dt = LAYERS[layer]
@@ -238,7 +245,7 @@ def test_what_a_row_does_not_see(layer):
     bt["vp"][bt["table"][4, 250 // 16], 250 % 16] = np.nan
     bt["table"][4, 2], bt["table"][4, 7], bt["table"][4, 0] = -1, len(bt["kp"]), -2 ** 31
     bt["table"][1, :] = -1
-    ctx = make_ctx(LAYERS[layer])
+    ctx = make_ctx(LAYERS[layer], kernel=kernel)
     out, lse = run_attn(ctx, bt)
     o = [int(x) for x in bt["offs"]]
     clean = {t for t in range(o[0], o[1]) if 100 + t < 120} | set(range(o[1], o[4])) | {o[4] + t for t in range(90) if 200 + t < 250}
@@ -251,8 +258,8 @@ def test_what_a_row_does_not_see(layer):
     ctx.close()
 
 
-@pytest.mark.parametrize("layer", ["g4", "g2_d64", "f32_d64"])
-def test_large_and_growing_logits(layer):
+@pytest.mark.parametrize("kernel,layer", FEW)
+def test_large_and_growing_logits(kernel, layer):
     """The largest logits come late, hundreds above the first: whatever reference the weights have, they keep their size."""
     Hq, Hkv, d, dt = LAYERS[layer]
     bt = make_batch(LAYERS[layer], [(900, 1), (300, 80), (2000, 1), (500, 300)], 16, seed=9, q_scale=4.0)
@@ -260,16 +267,16 @@ def test_large_and_growing_logits(layer):
         for j in range(c + n):
             bt["kp"][bt["table"][b, j // 16], j % 16] *= 1 + 9.0 * (j / (c + n)) ** 3
     bt["kp"] = stored(np.nan_to_num(bt["kp"], nan=0.0), dt) + np.where(np.isnan(bt["kp"]), np.float32(np.nan), np.float32(0))
-    ctx = make_ctx(LAYERS[layer])
+    ctx = make_ctx(LAYERS[layer], kernel=kernel)
     out, lse = run_attn(ctx, bt)
     check_attn(bt, out, lse, set(range(0, 382, 11)) | {0, 1, 80, 81, 82, 381})
     ctx.close()
 
 
-@pytest.mark.parametrize("layer", ["g4", "f32_d64"])
-def test_rows_beyond_max_new_and_a_narrow_table(layer):
+@pytest.mark.parametrize("kernel,layer", [("auto", "g4"), ("tiled", "g4"), ("auto", "f32_d64")])
+def test_rows_beyond_max_new_and_a_narrow_table(kernel, layer):
     bt = make_batch(LAYERS[layer], [(10, 50), (5, 1)], 16, seed=2)
-    ctx = make_ctx(LAYERS[layer])
+    ctx = make_ctx(LAYERS[layer], kernel=kernel)
     want, _ = run_attn(ctx, bt)
     out, _ = run_attn(ctx, bt, max_new=20)
     assert torch.equal(out[:20], want[:20]) or np.allclose(down(out[:20]), down(want[:20]), atol=2 * UBF * 4)   # (another kernel may take them)
@@ -280,7 +287,8 @@ def test_rows_beyond_max_new_and_a_narrow_table(layer):
     ctx.close()
 
 
-def test_offsets_beyond_32_bits():
+@pytest.mark.parametrize("kernel", ["stream", "tiled"])
+def test_offsets_beyond_32_bits(kernel):
     """Pages at the end of a cache of more than 2^32 bytes, and a row index beyond 2^31 elements."""
     layer = (8, 8, 128, "bf16")
     n_pages, page = 150000, 16                                        # 4.9 GB each
@@ -289,7 +297,7 @@ def test_offsets_beyond_32_bits():
     used = bt["kp"].shape[0]
     kp[-used:], vp[-used:] = up(bt["kp"], "bf16"), up(bt["vp"], "bf16")
     table = np.where(bt["table"] >= 0, bt["table"] + n_pages - used, -1)
-    ctx = make_ctx(layer)
+    ctx = make_ctx(layer, kernel=kernel)
     q, out = up(bt["q"], "bf16"), torch.zeros(bt["q"].shape, dtype=torch.bfloat16, device="cuda")
     lse = torch.zeros(bt["q"].shape[:2], device="cuda")
     ctx.fr_paged_attn(q, i32(bt["offs"]), i32(bt["cached"]), 2, 101, 100, kp, vp, n_pages, page, i32(table), table.shape[1], out, lse)
@@ -300,21 +308,23 @@ def test_offsets_beyond_32_bits():
     ctx.close()
 
 
-def test_many_requests_and_empty_ones():
+@pytest.mark.parametrize("kernel", ["auto", "tiled"])
+def test_many_requests_and_empty_ones(kernel):
     rng = np.random.default_rng(8)
     lens = [(int(rng.integers(0, 40)), int(rng.integers(0, 3))) for _ in range(1500)]
     bt = make_batch((2, 1, 64, "bf16"), lens, 8, seed=4)
-    ctx = make_ctx(bt["layer"])
+    ctx = make_ctx(bt["layer"], kernel=kernel)
     out, lse = run_attn(ctx, bt)
     check_attn(bt, out, lse, set(range(0, len(bt["q"]), 17)) | {len(bt["q"]) - 1})
     ctx.close()
 
 
-def test_a_prompt_in_one_call_and_in_chunks():
+@pytest.mark.parametrize("kernel", ["auto", "tiled"])
+def test_a_prompt_in_one_call_and_in_chunks(kernel):
     """2500 positions at once, and the same as chunks of 900 behind one another: sampled rows against the oracle, the two against each other."""
     layer = (8, 2, 128, "bf16")
     bt = make_batch(layer, [(0, 2500)], 64, seed=6)
-    ctx = make_ctx(layer)
+    ctx = make_ctx(layer, kernel=kernel)
     out, lse = run_attn(ctx, bt)
     check_attn(bt, out, lse, {0, 1, 63, 64, 65, 255, 256, 257, 1000, 1777, 2498, 2499})
     for c in range(0, 2500, 900):
@@ -323,6 +333,34 @@ def test_a_prompt_in_one_call_and_in_chunks():
         o, l = run_attn(ctx, part)
         assert np.allclose(down(o), down(out[c: c + n]), atol=2 * UBF * 4, rtol=0) and np.allclose(down(l), down(lse[c: c + n]), atol=1e-4)
     ctx.close()
+
+
+@pytest.mark.parametrize("lens,pad_blocks", [([(700, 400), (300, 1)], 600), ([(100, 300)] * 3 + [(2000, 1)] * 30, 0), ([(6000, 900)], 0), ([(3000, 700), (9, 1)], 400)])
+def test_both_kernels_in_a_call(lens, pad_blocks):
+    """Sizes on both sides of the rule, tables as wide as they need to be and wider (the kernels then find out which of them works): the
+    same rows as either kernel alone gives, up to their roundings, whatever the rule says."""
+    layer = (32, 8, 128, "bf16")
+    rng = np.random.default_rng(0)
+    need = [-(-(c + n) // 16) for c, n in lens]
+    n_pages, T = sum(need) + 1, sum(n for _, n in lens)
+    ids, at = rng.permutation(n_pages), 0
+    table = np.full((len(lens), max(need) + pad_blocks), -1)
+    for b, k in enumerate(need):
+        table[b, :k] = ids[at: at + k]
+        at += k
+    f = lambda *s: torch.randn(s, generator=torch.Generator(device="cuda").manual_seed(len(s) * sum(s)), device="cuda").bfloat16()
+    dev = dict(q=f(T, 32, 128), kp=f(n_pages, 16, 8, 128), vp=f(n_pages, 16, 8, 128) * 0.5, offs=i32(np.concatenate([[0], np.cumsum([n for _, n in lens])])),
+               cached=i32([c for c, _ in lens]), table=i32(table))
+    bt = dict(layer=layer, page=16, table=table, kp=dev["kp"], cached=lens, q=np.empty((T, 32, 0)), max_new=max(n for _, n in lens))
+    got = {}
+    for kernel in ("auto", "stream", "tiled"):
+        ctx = make_ctx(layer, kernel=kernel)
+        got[kernel] = [x.clone() for x in run_attn(ctx, bt, dev=dev)]
+        ctx.close()
+    for kernel in ("stream", "tiled"):
+        # two roundings of each weight, two of each output, of values of at most 3 (the weights' mean of |value| is 0.4)
+        assert float((got["auto"][0].float() - got[kernel][0].float()).abs().max()) <= 4 * UBF * 3
+        assert float((got["auto"][1] - got[kernel][1]).abs().max()) <= 1e-4
 
 
 # ---- the step ------------------------------------------------------------------------------------------------------------

@@ -56,6 +56,16 @@ def test_attention_refusals(ctx, status, change):
     refused(status, ctx.fr_paged_attn, ATTN, **change)
 
 
+def test_rows_times_heads_stay_below_two_to_the_31(ctx):
+    refused(UNS, ctx.fr_paged_attn, ATTN, n_tokens=2 ** 28)         # eight heads
+
+
+def test_option_values(ctx):
+    for v in (B.FR_PAGED_KERNEL_AUTO, B.FR_PAGED_KERNEL_STREAM, B.FR_PAGED_KERNEL_TILED):
+        ctx.fr_set_option(B.FR_OPT_PAGED_KERNEL, v)
+    refused(ARG, ctx.fr_set_option, dict(option=B.FR_OPT_PAGED_KERNEL), value=3)
+
+
 def test_nothing_to_do(ctx):
     ctx.fr_paged_append(**{**APPEND, "n_tokens": 0, "k_new": None, "slots": None})
     for none in ("n_tokens", "n_requests", "max_new"):
