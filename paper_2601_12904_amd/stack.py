@@ -86,7 +86,9 @@ class SelectivePrefillStack:
 
 class PagedCache:
     """K/V of up to `n_requests` requests in pages of `page_rows` rows, for every layer; one free list and one block table serve all layers.
-    Lengths and tables stay on the device (a captured step serves other lengths)."""
+    Lengths and tables stay on the device (a captured step serves other lengths).  A step that asks for more pages than the list has
+    leaves the rows without one out of the cache: `free_start` is beyond `n_pages` then.  A request that ends is taken out by its
+    length 0 and new entries of `free_pages`; the list may be rewritten between steps."""
 
     def __init__(self, n_layers: int, n_requests: int, n_pages: int, page_rows: int, max_blocks: int, Hkv: int, d: int,
                  dtype=torch.bfloat16):
@@ -112,16 +114,22 @@ class PagedStack:
         self.Hq, self.Hkv, self.d = d.n_q_heads, d.n_kv_heads, d.head_dim
         # fr_qkv_rope rotates rows of this layout itself; others are projected part by part and rotated on the way into the pages
         self.fused_rope = d.head_dim == 128 and d.rope_layout == B.FR_ROPE_INTERLEAVED
-        self._buf = {}
+        self._buf, self._captured = {}, []
 
     def _scratch(self, T: int, n: int):
-        if self._buf.get("key") != (T, n):
-            mk = lambda *shape: torch.empty(shape, dtype=torch.bfloat16, device="cuda")
-            i32 = lambda m: torch.empty(m, dtype=torch.int32, device="cuda")
-            self._buf = dict(key=(T, n), x=mk(T, self.hidden), q=mk(T, self.Hq, self.d), k=mk(T, self.Hkv, self.d), v=mk(T, self.Hkv, self.d),
-                             attn=torch.zeros((T, self.Hq, self.d), dtype=torch.bfloat16, device="cuda"), act=mk(T, self.ffn),
-                             offsets=i32(n + 1), positions=i32(T), slots=i32(T))
-        return self._buf
+        capturing = torch.cuda.is_current_stream_capturing()
+        if not capturing and self._buf.get("key") == (T, n):
+            return self._buf
+        mk = lambda *shape: torch.empty(shape, dtype=torch.bfloat16, device="cuda")
+        i32 = lambda m: torch.empty(m, dtype=torch.int32, device="cuda")
+        buf = dict(key=(T, n), x=mk(T, self.hidden), q=mk(T, self.Hq, self.d), k=mk(T, self.Hkv, self.d), v=mk(T, self.Hkv, self.d),
+                   attn=torch.zeros((T, self.Hq, self.d), dtype=torch.bfloat16, device="cuda"), act=mk(T, self.ffn),
+                   offsets=i32(n + 1), positions=i32(T), slots=i32(T))
+        if capturing:
+            self._captured.append(buf)   # a graph's own, for as long as the stack lives: steps of other sizes do not free it
+        else:
+            self._buf = buf
+        return buf
 
     def forward(self, h: torch.Tensor, new_len: torch.Tensor, max_new: int, cache: PagedCache) -> torch.Tensor:
         """h [T, hidden] is updated in place and returned: the requests' rows one after the other, rows behind them hold nothing of use.

@@ -413,10 +413,10 @@ def test_steps_against_the_oracle(layer):
     ctx.close()
 
 
-@pytest.mark.parametrize("layer", ["g4", "f32_d64"])
-def test_a_captured_step_is_replayed_for_other_lengths(layer):
-    ctx, s = make_ctx(LAYERS[layer]), _step_case(LAYERS[layer], 2)
-    other_ctx, e = make_ctx(LAYERS[layer]), _step_case(LAYERS[layer], 2)
+@pytest.mark.parametrize("kernel,layer", [("auto", "g4"), ("auto", "f32_d64"), ("tiled", "g4")])
+def test_a_captured_step_is_replayed_for_other_lengths(kernel, layer):
+    ctx, s = make_ctx(LAYERS[layer], kernel=kernel), _step_case(LAYERS[layer], 2)
+    other_ctx, e = make_ctx(LAYERS[layer], kernel=kernel), _step_case(LAYERS[layer], 2)
     _step(ctx, s)                                             # once eagerly, on both
     _step(other_ctx, e)
     torch.cuda.synchronize()
@@ -488,3 +488,46 @@ def test_stack_in_steps_equals_the_stack_at_once(d, half):
     assert float((got.float() - whole.float()).abs().max()) <= 10 * L * UBF * size
     assert torch.isfinite(got.float()).all()
     ctx.close()
+
+
+def test_captured_stack_steps_beside_eager_ones():
+    """Two captured steps of one stack (a decoding step, a chunk) and eager steps of other sizes between their replays: the rows of
+    the same steps taken eagerly."""
+    Hq, Hkv, d, hidden, ffn, L, n = 8, 2, 128, 512, 256, 2, 3
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    layers = [S.random_layer(hidden, ffn, Hq, Hkv, d, gen, std=0.05) for _ in range(L)]
+    x = torch.randn((400, hidden), generator=gen, device="cuda").bfloat16()
+    results = []
+    for captured in (False, True):
+        ctx = make_ctx((Hq, Hkv, d, "bf16"), tokens=256)
+        stack = S.PagedStack(ctx, layers, hidden, ffn)
+        cache = S.PagedCache(L, n, 60, 8, 16, Hkv, d)
+        graphs = {}
+        if captured:
+            for T in (n, 48):
+                h, new = torch.zeros((T, hidden), device="cuda").bfloat16(), i32([0] * n)
+                stack.forward(h, new, T, cache)      # (once outside: the library's first calls set up what a capture may not; no rows)
+                torch.cuda.synchronize()
+                g = torch.cuda.CUDAGraph()
+                with torch.cuda.graph(g):
+                    stack.forward(h, new, T, cache)
+                graphs[T] = g, h, new
+        got, at = [], 0
+        for new in ([20, 0, 28], [1, 1, 1], [30, 5, 7], [1, 0, 1], [10, 20, 18], [1, 1, 1]):
+            T = n if max(new) == 1 else 48 if new != [30, 5, 7] else 50      # (50 rows: always eager)
+            rows = x[at: at + T].clone()
+            at += sum(new)
+            if T in graphs:
+                g, h, dev_new = graphs[T]
+                h.copy_(rows)
+                dev_new.copy_(i32(new))
+                g.replay()
+                torch.cuda.synchronize()
+                rows = h.clone()
+            else:
+                stack.forward(rows, i32(new), T, cache)
+            got.append(rows[: sum(new)])
+        assert cache.cached_len.tolist() == [63, 27, 56]
+        results.append(torch.cat(got))
+        ctx.close()
+    assert torch.isfinite(results[0].float()).all() and torch.equal(results[0], results[1])
