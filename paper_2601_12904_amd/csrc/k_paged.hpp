@@ -63,16 +63,12 @@ __device__ __forceinline__ int64_t uniform64(int64_t v) {
     return (int64_t)(((uint64_t)hi << 32) | lo);
 }
 
-// How a launch's work is dealt out.  The work of a KV head is one line of units: requests in order, of each its column tiles, of each its units of keys.
-// Workgroup w of n takes units floor(w U / n) .. floor((w + 1) U / n) - 1 of it, wherever they begin and end, so every workgroup has the same
-// share whatever the lengths are, and the host need not know them.  n is at most U (paged_sharers): none of them goes without.  That one also
-// leaves a PagedCut, which is all that the joining pass has to read to find its work.  An item (column tile) that falls to several workgroups leaves a partial result
-// per piece: in slot 2 w of a workgroup whose piece begins behind the item's start, in 2 w + 1 of the one that has its start but not its end.
 // blockIdx.x = workgroup of the KV head x Hkv + KV head: blocks go to the eight dies in turn, so that with 8 KV heads each die's cache serves one of them.
 __device__ __forceinline__ int paged_head(const PagedArgs& a) { return blockIdx.x % a.Hkv; }
 __device__ __forceinline__ int paged_workgroup(const PagedArgs& a) { return blockIdx.x / a.Hkv; }
 inline unsigned paged_grid(int64_t workgroups, int Hkv) { return (unsigned)(workgroups * Hkv); }
-// Do the requests with many columns go through the tiled kernel?  It takes 45 us for the first key tile of every request and 1.5 us for 256 columns x 64 keys on a
+
+// Do the requests with many columns go through the tiled kernel?  It takes 34 us for the shortest call and 1.5 us for 256 columns x 64 keys on a
 // compute unit, the streaming kernel 11 us and twice the time per column, and it reads the keys again for every 32 columns, from the die's cache as
 // long as they fit about twice.  us tiled : streaming, rows behind positions (columns x keys of all KV heads); 32 / 8 heads: 128 behind 1000 (5 M) 58 : 23, 512 behind 4000 (74 M) 103 : 68,
 // 512 behind 14336 (243 M) 167 : 196, 1024 from nothing (34 M) 63 : 42, 2048 (134 M) 90 : 112; 64 / 8 heads: 512 behind 4000 (148 M) 128 : 126, 128 behind 14336 (118 M) 98 : 110;
@@ -98,6 +94,11 @@ __device__ __forceinline__ bool paged_route(const PagedArgs& a, int row_bytes) {
     return pairs * a.Hkv > (keys * row_bytes <= PAGED_NEAR_BYTES ? PAGED_PAIRS_NEAR : PAGED_PAIRS_FAR) >> 10;
 }
 
+// How a launch's work is dealt out.  The work of a KV head is one line of units: requests in order, of each its column tiles, of each its units of keys.
+// Workgroup w of n takes units floor(w U / n) .. floor((w + 1) U / n) - 1 of it, wherever they begin and end, so every workgroup has the same
+// share whatever the lengths are, and the host need not know them.  n is at most U (paged_sharers): none of them goes without.  An item (column tile) that falls to several
+// workgroups leaves a partial result per piece: in slot 2 w of a workgroup whose piece begins behind the item's start, in 2 w + 1 of the one that has its start but not its
+// end.  That one also leaves a PagedCut, which is all that the joining pass has to read to find its work.
 struct alignas(16) PagedCut {   // of a workgroup and KV head; in front of the partial results
     int pieces;      // of the item that it has the start but not the end of: its own and those of the workgroups behind it; 0: there is no such item
     int first_row;   // of the request

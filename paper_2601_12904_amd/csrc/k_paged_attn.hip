@@ -6,7 +6,7 @@
 // Which kernels a call takes.  The lengths are on the device; the host knows the number of requests and rows and a bound on the rows of one.  A request with few query columns
 // (rows x heads of a group) is bound by the bytes of its keys and values: k_paged_stream.hip; one with many by the matrix instructions: k_paged_tile.hip, whose
 // tile of 256 columns takes 1.5 us per 64 keys however few of them there are.  Where the total decides and the host's bounds do not (a table has room for more than
-// its requests hold), both are launched and find out which of them works (paged_route); the other one's launch and its joining pass take 9 us.
+// its requests hold), both are launched and find out which of them works (paged_route); the other one's launch and its joining pass take 9.5 us.
 #include "k_paged.hpp"
 
 #include <algorithm>

@@ -4,11 +4,12 @@
 // n_b = off[b + 1] - off[b], from the free list behind those of the requests before it; row t of request b is position c_b + t - off[b].  A launch
 // of one kernel is all there is to it: every workgroup scans the lengths of all requests itself (16 KB at most, in the caches) rather than
 // wait for a pass that does, then every thread finds the request of its row, and of its page, by bisection in LDS.  The pages of a row are looked up
-// in the free list, not in the table that other threads are writing.
+// in the free list, not in the table that other threads are writing.  Latency: 4.4 us for 64 requests of a row each, 5.3 for 256 that bring 13 668; a launch of nothing is 4.
 //
 // Append.  One wave per row: its lanes form the row's (cos, sin) pairs in fp64, rounded once, while the row's vectors are on their way, and then take
 // vectors v and v + NV / 2 of a head together, which are a pair's two halves in the half-split layout, so that q may be rotated in place.
 // Streaming: bound by memory for long prompts, by the chain positions -> angle -> store for a decoding step.
+// 16896 rows of 32 / 8 heads 79 us = 5.25 TB/s read and written (a device copy of 1 GiB 5.09); 64 rows 3.8 us, 2640 rows of 16 / 8 heads of 64 5.7.
 #include "k_rotate.hpp"
 
 #include <algorithm>

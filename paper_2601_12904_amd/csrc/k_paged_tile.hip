@@ -24,6 +24,10 @@
 // keys, found in a pass over them that forms nothing but logits.  Weights go into the second product as bf16 (half a step, 2^-8, of each; their sum is
 // taken in fp32 before), as the output does.
 //
+// Bound by the matrix instructions and the power they take: 3095 cycles per tile of 64 keys, 2048 of them matrix instructions of each SIMD, at 1.7 - 1.9 GHz under full load.  2048 rows
+// behind 14336 (32 / 8 heads, head_dim 128) 441 us = 1.17 PFLOP/s, 16896 from nothing 2004 us = 1.17 PFLOP/s; a library product of 8192^3 reaches 1.20.  An item takes
+// 17 us beside its tiles: plan, queries and page numbers 9, first copies and references 3, exchange and output 5.
+//
 // What a column does not see stays out of it by hand, as a weight of 0 does not take a NaN or an infinity out of a product: keys behind the tile's last row
 // repeat that one; a value that is not finite and that some column does not see makes that one's sums NaN, and in the second go the wave that brought a
 // row of such a tile takes values that are not finite out of LDS; they reach the columns that see them when the loop is over.
