@@ -934,6 +934,9 @@ fr_status fr_paged_attn(fr_ctx* ctx, const void* q, const int32_t* q_offsets, co
     if (bad4(q_offsets) || bad4(cached_len) || (max_blocks > 0 && bad4(block_table)))
         return fail(ctx, FR_ERR_INVALID_ARG, "q_offsets / cached_len / block_table is NULL or not 4-byte aligned");
     if (reinterpret_cast<uintptr_t>(lse_out) & 3u) return fail(ctx, FR_ERR_INVALID_ARG, "lse_out must be 4-byte aligned");
+    const int64_t q_bytes = (int64_t)n_tokens * ctx->shape.Hq * ctx->shape.d * ctx->shape.esize;
+    if (q != out && (const char*)q < (const char*)out + q_bytes && (const char*)out < (const char*)q + q_bytes)
+        return fail(ctx, FR_ERR_INVALID_ARG, "q and out overlap without being equal");
     if ((st = need_device(ctx)) != FR_OK) return st;
     PagedAttnArgs a{};
     a.q = q; a.q_offsets = q_offsets; a.cached_len = cached_len; a.n_requests = n_requests; a.n_tokens = n_tokens;

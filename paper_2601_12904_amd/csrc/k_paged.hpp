@@ -98,7 +98,8 @@ __device__ __forceinline__ bool paged_route(const PagedArgs& a, int row_bytes) {
 // Workgroup w of n takes units floor(w U / n) .. floor((w + 1) U / n) - 1 of it, wherever they begin and end, so every workgroup has the same
 // share whatever the lengths are, and the host need not know them.  n is at most U (paged_sharers): none of them goes without.  An item (column tile) that falls to several
 // workgroups leaves a partial result per piece: in slot 2 w of a workgroup whose piece begins behind the item's start, in 2 w + 1 of the one that has its start but not its
-// end.  That one also leaves a PagedCut, which is all that the joining pass has to read to find its work.
+// end.  The one with the start also leaves a PagedCut, which is all that the joining pass has to read to find its work.  A query column is read by the workgroups of its item
+// alone, and its output is stored when they have read it: out may be q.
 struct alignas(16) PagedCut {   // of a workgroup and KV head; in front of the partial results
     int pieces;      // of the item that it has the start but not the end of: its own and those of the workgroups behind it; 0: there is no such item
     int first_row;   // of the request

@@ -133,7 +133,8 @@ class PagedStack:
 
     def forward(self, h: torch.Tensor, new_len: torch.Tensor, max_new: int, cache: PagedCache) -> torch.Tensor:
         """h [T, hidden] is updated in place and returned: the requests' rows one after the other, rows behind them hold nothing of use.
-        new_len [n_requests] int32 on the device, none beyond max_new.  The cache's lengths and free list move on."""
+        new_len [n_requests] int32 on the device, none beyond max_new.  With head_dim 128 and interleaved pairs T is at most the
+        context's max_tokens (fr_qkv_rope).  The cache's lengths and free list move on."""
         c, T, n = self.ctx, h.shape[0], cache.n_requests
         s = self._scratch(T, n)
         c.fr_page_tables(cache.cached_len, new_len, n, cache.page_rows, cache.free_pages, cache.n_pages, cache.free_start, cache.block_table,

@@ -308,6 +308,36 @@ def test_offsets_beyond_32_bits(kernel):
     ctx.close()
 
 
+@pytest.mark.parametrize("kernel,layer", FEW)
+@pytest.mark.parametrize("form", ["decode", "one_long", "mixed", "few_behind_many"])
+def test_outputs_in_the_place_of_the_queries(kernel, layer, form):
+    """Whole items, cut ones and (logits that outgrow the first keys') items that are taken twice."""
+    bt = make_batch(LAYERS[layer], FORMS[form], 16, seed=3)
+    ctx = make_ctx(LAYERS[layer], kernel=kernel)
+    for scale in (1.0, 100.0):
+        dt = LAYERS[layer][3]
+        dev = dict(q=up(bt["q"] * scale, dt), kp=up(bt["kp"], dt), vp=up(bt["vp"], dt), offs=i32(bt["offs"]), cached=i32(bt["cached"]), table=i32(bt["table"]))
+        want, _ = run_attn(ctx, bt, dev=dev)
+        q = dev["q"]
+        ctx.fr_paged_attn(q, dev["offs"], dev["cached"], len(bt["cached"]), len(bt["q"]), bt["max_new"], dev["kp"], dev["vp"], len(bt["kp"]), bt["page"], dev["table"],
+                          bt["table"].shape[1], q)
+        n = int(bt["offs"][-1])
+        assert torch.equal(q[:n], want[:n])
+    ctx.close()
+
+
+@pytest.mark.parametrize("kernel", ["auto", "tiled"])
+@pytest.mark.parametrize("heads", [(130, 1), (320, 320), (96, 2)])
+def test_wide_groups_and_many_heads(kernel, heads):
+    """A group wider than a tile of the streaming kernel and than half of the tiled one's, more KV heads than compute units."""
+    layer = heads + (64, "bf16")
+    bt = make_batch(layer, [(300, 3), (0, 1), (70, 9)], 16, seed=heads[0])
+    ctx = make_ctx(layer, kernel=kernel)
+    out, lse = run_attn(ctx, bt)
+    check_attn(bt, out, lse)
+    ctx.close()
+
+
 @pytest.mark.parametrize("kernel", ["auto", "tiled"])
 def test_many_requests_and_empty_ones(kernel):
     rng = np.random.default_rng(8)

@@ -60,6 +60,11 @@ def test_rows_times_heads_stay_below_two_to_the_31(ctx):
     refused(UNS, ctx.fr_paged_attn, ATTN, n_tokens=2 ** 28)         # eight heads
 
 
+def test_outputs_on_top_of_queries_only_as_a_whole(ctx):
+    refused(ARG, ctx.fr_paged_attn, ATTN, out=P + 256)
+    refused(ARG, ctx.fr_paged_attn, ATTN, q=P + 256)
+
+
 def test_option_values(ctx):
     for v in (B.FR_PAGED_KERNEL_AUTO, B.FR_PAGED_KERNEL_STREAM, B.FR_PAGED_KERNEL_TILED):
         ctx.fr_set_option(B.FR_OPT_PAGED_KERNEL, v)
