@@ -73,7 +73,10 @@ inline unsigned paged_grid(int64_t workgroups, int Hkv) { return (unsigned)(work
 // long as they fit about twice.  us tiled : streaming, rows behind positions (columns x keys of all KV heads); 32 / 8 heads: 128 behind 1000 (5 M) 58 : 23, 512 behind 4000 (74 M) 103 : 68,
 // 512 behind 14336 (243 M) 167 : 196, 1024 from nothing (34 M) 63 : 42, 2048 (134 M) 90 : 112; 64 / 8 heads: 512 behind 4000 (148 M) 128 : 126, 128 behind 14336 (118 M) 98 : 110;
 // sixteen times 40 behind 3000: 32 / 8 heads (62 M, 25 MB per KV head) 107 : 168, head_dim 64 (31 M, 12 MB) 59 : 41.
+// Few keys make short items, which the tiled kernel takes whole, one for a workgroup: 30 us and 1.5 for 64 of its keys.  From nothing, 64 / 8 heads, 768 rows (38 M) 56 : 47, 900 (52 M) 59 : 72, 1024 (67 M)
+// 63 : 70, 1200 (92 M) 84 : 105; 600 behind 500 (42 M) 64 : 64, 512 behind 1000 (50 M) 70 : 51; 28 / 4 heads, 1200 (40 M) 65 : 57, 1500 (63 M) 73 : 75.
 constexpr int64_t PAGED_PAIRS_NEAR = 100000000, PAGED_PAIRS_FAR = 35000000;   // columns x keys; the keys of a KV head in PAGED_NEAR_BYTES, or more
+constexpr int64_t PAGED_PAIRS_SHORT = 24000000, PAGED_PAIRS_KEY = 29000;   // and near keys that are few: this, and this for each of them
 constexpr int64_t PAGED_NEAR_BYTES = 8 << 20;
 __device__ __forceinline__ bool paged_route(const PagedArgs& a, int row_bytes) {
     const int lane = threadIdx.x & 63;
@@ -91,7 +94,7 @@ __device__ __forceinline__ bool paged_route(const PagedArgs& a, int row_bytes) {
         pairs += uniform64(wave_sum64(p, min(64, a.B - b0)));
         keys += uniform64(wave_sum64(k, min(64, a.B - b0)));
     }
-    return pairs * a.Hkv > (keys * row_bytes <= PAGED_NEAR_BYTES ? PAGED_PAIRS_NEAR : PAGED_PAIRS_FAR) >> 10;
+    return pairs * a.Hkv > (keys * row_bytes <= PAGED_NEAR_BYTES ? min(PAGED_PAIRS_NEAR, PAGED_PAIRS_SHORT + PAGED_PAIRS_KEY * keys) : PAGED_PAIRS_FAR) >> 10;
 }
 
 // How a launch's work is dealt out.  The work of a KV head is one line of units: requests in order, of each its column tiles, of each its units of keys.

@@ -38,11 +38,11 @@ hipError_t launch_paged_attn(const Shape& s, const PagedAttnArgs& args, float* p
     a.cols_hi = INT32_MAX;
     if (args.kernel == FR_PAGED_KERNEL_TILED) return launch_paged_tile(s, a, n_cu, st);
     const int64_t rows = std::min<int64_t>(a.T, (int64_t)a.B * a.max_new);
-    // columns x keys of all KV heads (paged_route): no more than what the table has room for, no less than the chunks themselves
+    // columns x keys of all KV heads (paged_route): no more than what the table has room for, no less than the chunks themselves (rows of no request are taken for some's)
     const double most = (double)rows * s.Hq * a.cap, least = (double)rows * rows / a.B * s.Hq;
     if ((int64_t)args.max_new * s.G <= a.few || most <= (double)PAGED_PAIRS_FAR) return launch_paged_stream(s, a, n_cu, st);
     a.together = (int64_t)(args.n_requests - 1) * s.Hkv <= n_cu / 4;
-    a.route = least <= (double)PAGED_PAIRS_NEAR;
+    a.route = least <= std::min((double)PAGED_PAIRS_NEAR, PAGED_PAIRS_SHORT + (double)PAGED_PAIRS_KEY * a.B * a.cap);
     if (a.route || !a.together) {
         if (!a.route) a.cols_hi = a.few;
         hipError_t e = launch_paged_stream(s, a, n_cu, st);
