@@ -19,7 +19,8 @@
 // A wave copies a block global -> LDS (no registers, no wait) while it works on the one before.  The page numbers of a block's keys come the same way
 // one block earlier, so that the copies of a wave are the only thing its memory counter counts, and every page size goes the same way.
 //
-// Softmax.  A column's exponent reference goes up, and its sums are scaled, only when a logit is 8 (base 2) or more above it.
+// Softmax.  A column's exponent reference goes up, and its sums are scaled, only when a logit is 8 (base 2) or more above it.  A wave one of whose references
+// is PAGED_FAR or more rounds the scaled logits before it takes the reference from them.
 //
 // What a column does not see stays out of it by hand, as a weight of 0 does not take a NaN or an infinity out of a product: keys behind the tile's last
 // row repeat that one, and values that are not finite leave a block that only some columns see whole and reach those columns when the loop is over.
@@ -151,7 +152,7 @@ struct StreamPiece {
 #pragma unroll
             for (int i = 0; i < COPIES; ++i) paged_copy16(v_base + (size_t)row[i] * row_bytes + v_place, v_lds + 1024 * i);
         };
-        bool apart = false;
+        bool apart = false, far = false;   // far: some column's reference has reached PAGED_FAR
         int blk = W * r0 + wave;
         if (blk < n_blocks) {
             const int last = n_blocks - 1;   // (past the last block: that one again, nobody uses it; the counts of the waits stay the same)
@@ -235,7 +236,18 @@ struct StreamPiece {
                         l[nb] *= down;
 #pragma unroll
                         for (int md = 0; md < NJ; ++md) o[md][nb] *= down;
+                        far = far || __any(fabsf(up) >= PAGED_FAR && up != PAGED_NO_MAX);
                     }
+                }
+                const float scale = far ? 1.f : a.scale_log2e;
+                if (__builtin_expect(far, 0)) {
+#pragma clang fp contract(off)
+#pragma unroll
+                    for (int bb = 0; bb < 2; ++bb)
+#pragma unroll
+                        for (int nb = 0; nb < NC; ++nb)
+#pragma unroll
+                            for (int v = 0; v < 4; ++v) s[bb][nb][v] *= a.scale_log2e;
                 }
                 u32x4 p[NC];   // bf16: weights as the B operand of the second product: slot 4 bb + v of quarter kg is key 16 bb + 4 kg + v
 #pragma unroll
@@ -244,8 +256,8 @@ struct StreamPiece {
                     for (int bb = 0; bb < 2; ++bb)
 #pragma unroll
                         for (int v = 0; v < 4; v += 2) {
-                            const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[bb][nb][v], a.scale_log2e, -m[nb]));
-                            const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[bb][nb][v + 1], a.scale_log2e, -m[nb]));
+                            const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[bb][nb][v], scale, -m[nb]));
+                            const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[bb][nb][v + 1], scale, -m[nb]));
                             l[nb] += p0 + p1;
                             if constexpr (F32) {
                                 s[bb][nb][v] = p0;

@@ -20,7 +20,7 @@
 //
 // Softmax.  exp(x - m) / sum exp(x - m) does not depend on m, and fp32 and bf16 leave about 2^127 of room, so a column's exponent reference is the maximum over its
 // visible ones of the request's keys 0..31, in every piece of its item, and the loop holds no maximum, no comparison and no rescaling (which would
-// spill registers).  Where the sums show that a later logit passed it by more than that, the piece is done again with the largest logit of its own
+// spill registers).  Where the sums show that a later logit passed it by more than that, or where it is PAGED_FAR or more, the piece is done again with the largest logit of its own
 // keys, found in a pass over them that forms nothing but logits.  Weights go into the second product as bf16 (half a step, 2^-8, of each; their sum is
 // taken in fp32 before), as the output does.
 //
@@ -287,7 +287,7 @@ __device__ __forceinline__ void matrix_phase(uint32_t tv, uint32_t tk, const bf1
 
 // Key tiles [kb, ke) of an item.  whole: they are all it has, the outputs are stored; else the partial result goes to `part`: [C][2] references and sums,
 // then [C][D] weighted values.
-// EXACT = false: returns false where the sums overflowed the reference or are NaN, or where keys 0..31 have none; what it stored is worth nothing then, and the caller does
+// EXACT = false: returns false where the sums overflowed the reference or are NaN, where the reference is far from 0, or where keys 0..31 have none; what it stored is worth nothing then, and the caller does
 // the piece again with EXACT = true.
 template <int D, bool ALIGNED, bool EXACT>
 __device__ __forceinline__ bool process_piece(const PagedArgs& a, const PagedRequest& rq, int b, int t, int g, int kb, int ke, bool whole, float* part,
@@ -578,6 +578,10 @@ __device__ __forceinline__ bool process_piece(const PagedArgs& a, const PagedReq
             c0 = c1; c1 = c2; c2 = vp;
             __builtin_amdgcn_sched_barrier(0);
         };
+        auto above = [&](float logit, float reference) {   // logit x scale - reference (EXACT: of the rounded product, PAGED_FAR)
+#pragma clang fp contract(off)
+            return EXACT ? logit * a.scale_log2e - reference : __builtin_fmaf(logit, a.scale_log2e, -reference);
+        };
         auto softmax = [&](int kt, int ahead) {   // and the rows of tile `ahead`, which the copies behind it, or the next ones, do not bring yet
             const Rows found = find_rows(ahead, ahead & 7);
             uint32_t hole = 0;
@@ -591,8 +595,8 @@ __device__ __forceinline__ bool process_piece(const PagedArgs& a, const PagedReq
                 for (int bb = 0; bb < 2; ++bb)
 #pragma unroll
                     for (int v = 0; v < 4; v += 2) {
-                        const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[bb][nb][v], a.scale_log2e, -m[nb]));
-                        const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[bb][nb][v + 1], a.scale_log2e, -m[nb]));
+                        const float p0 = __builtin_amdgcn_exp2f(above(s[bb][nb][v], m[nb]));
+                        const float p1 = __builtin_amdgcn_exp2f(above(s[bb][nb][v + 1], m[nb]));
                         s0 = bb == 0 && v == 0 ? p0 : s0 + p0;
                         s1 = bb == 0 && v == 0 ? p1 : s1 + p1;
                         bf16x2 w;
@@ -723,7 +727,8 @@ __device__ __forceinline__ bool process_piece(const PagedArgs& a, const PagedReq
             for (int md = 0; md < MH; ++md)
 #pragma unroll
                 for (int v = 0; v < 4; ++v) check += fabsf(oh[md][nb][v]);
-            bad = bad || !(check < limit);
+            const float ref = refs[nb];
+            bad = bad || !(check < limit) || (fabsf(ref) >= PAGED_FAR && ref != PAGED_NO_MAX);
         }
         if (any_of_workgroup(bad, answers + WAVES)) return false;   // (also: the exchange has been read)
     } else {
