@@ -378,7 +378,8 @@ fr_status fr_paged_append(fr_ctx* ctx, const void* q, const void* k_new, const v
  *   out          dev [n_tokens, Hq, d]; may equal q;  lse_out dev [n_tokens, Hq] fp32 natural-log normalisers, or NULL
  * Rows of no request (q_offsets[n_requests] .. n_tokens - 1) are left as they were.  A position whose table entry is not a page
  * of the cache (0 .. n_pages - 1), or that lies beyond max_blocks pages, is invisible; a row that sees nothing at all (also: at a
- * negative position) has out = 0 and lse = -inf.  What a row does not see has no influence on it, whatever it holds.
+ * negative position) has out = 0 and lse = -inf, as has one whose logits are all -inf.  Every finite logit counts.  What a row does not see has no
+ * influence on it, whatever it holds.
  * Arithmetic: products of dtype inputs accumulated in fp32, softmax in fp32, out rounded to dtype. */
 fr_status fr_paged_attn(fr_ctx* ctx, const void* q, const int32_t* q_offsets, const int32_t* cached_len, int32_t n_requests,
                         int32_t n_tokens, int32_t max_new, const void* k_pages, const void* v_pages, int32_t n_pages,

@@ -162,7 +162,7 @@ typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
-constexpr float PAGED_NO_MAX = -1.0e30f;   // exponent reference of a column that has seen nothing
+constexpr float PAGED_NO_MAX = -3.402823466e38f;   // exponent reference of a column that has seen nothing: below every finite logit times the scale (0.18 at most)
 constexpr float PAGED_RAISE = 8.f;         // a column's reference goes up when a logit is this far (base 2) above it: weights stay below 2^8
 // References of this size (base 2) and more: the reference is a rounded product (logit x scale), and a multiply-add that subtracts it sees the product before its rounding, up to half a
 // step of the reference away, which is a factor of 2 in the weights at 2^24, and from 2^31 on infinity, or 0 for the largest logit itself.  There the products are rounded first.

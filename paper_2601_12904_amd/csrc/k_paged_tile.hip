@@ -460,7 +460,7 @@ __device__ __forceinline__ bool process_piece(const PagedArgs& a, const PagedReq
             asm volatile("" ::: "memory");
         };
         if constexpr (EXACT) {   // the maximum of its logits over the piece's visible keys
-            f32x4 top = {PAGED_NO_MAX, PAGED_NO_MAX, PAGED_NO_MAX, PAGED_NO_MAX};
+            f32x4 top = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
             store_q();
             prime(false);
             paged_wait_but<0>();
@@ -492,7 +492,7 @@ __device__ __forceinline__ bool process_piece(const PagedArgs& a, const PagedReq
 #pragma unroll
             for (int nb = 0; nb < NC; ++nb) {
                 const float t = fmaxf(top[nb], sm.ref[wave ^ 4][16 * nb + x]);
-                if (!second && kg == 0) refs[nb] = t == PAGED_NO_MAX ? PAGED_NO_MAX : t * a.scale_log2e;
+                if (!second && kg == 0) refs[nb] = fmaxf(t * a.scale_log2e, PAGED_NO_MAX);
             }
             prime(true);
 #pragma unroll

@@ -79,3 +79,32 @@ def test_logits_far_apart(kernel, layer, exponent, where, sign):
     decided, total = check(bt, out, lse, rows)
     assert decided > 0.9 * total, (decided, total)
     ctx.close()
+
+
+@pytest.mark.parametrize("kernel,layer", FEW)
+@pytest.mark.parametrize("where,sign", [("all", 0), ("all", 1), ("all", -1), ("late", 0), ("late", -1), ("early", -1)])
+@pytest.mark.parametrize("exponent", [100, 112])
+def test_logits_beyond_1e30(kernel, layer, exponent, where, sign):
+    """A finite logit is seen, however low it is."""
+    test_logits_far_apart(kernel, layer, exponent, where, sign)
+
+
+@pytest.mark.parametrize("kernel,layer", FEW)
+def test_logits_of_minus_infinity(kernel, layer):
+    """Rows all of whose logits are -infinity, and rows with one finite logit among such."""
+    dt = LAYERS[layer][3]
+    bt = make_batch(LAYERS[layer], [(300, 70), (40, 1), (0, 20), (900, 1)], 16, seed=8)
+    bt["q"] = stored(np.abs(bt["q"]) + 0.5, dt)
+    for b, (c, n) in enumerate([(300, 70), (40, 1), (0, 20), (900, 1)]):
+        for j in range(c + n):
+            if (b, j) not in ((0, 310), (2, 5), (3, 33)):
+                bt["kp"][bt["table"][b, j // 16], j % 16] = -np.inf
+    ctx = make_ctx(LAYERS[layer], kernel=kernel)
+    out, lse = (down(x) for x in run_attn(ctx, bt))
+    blind = [*range(0, 10), 70, *range(71, 76)]
+    assert np.all(out[blind] == 0) and np.all(np.isneginf(lse[blind]))
+    seen = {0: (range(10, 70), 310), 2: (range(76, 91), 5), 3: (range(91, 92), 33)}
+    for b, (rows, j) in seen.items():
+        v = bt["vp"][bt["table"][b, j // 16], j % 16].repeat(LAYERS[layer][0] // LAYERS[layer][1], axis=0)
+        assert np.all(np.abs(out[list(rows)] - v) <= (UBF if dt == "bf16" else 4 * U32) * np.abs(v)) and np.all(np.isfinite(lse[list(rows)]))
+    ctx.close()
