@@ -380,6 +380,8 @@ fr_status fr_paged_append(fr_ctx* ctx, const void* q, const void* k_new, const v
  * of the cache (0 .. n_pages - 1), or that lies beyond max_blocks pages, is invisible; a row that sees nothing at all (also: at a
  * negative position) has out = 0 and lse = -inf, as has one whose logits are all -inf.  Every finite logit counts.  What a row does not see has no
  * influence on it, whatever it holds.
+ * Rows of no request cost next to nothing themselves, but n_tokens and max_new also tell the host which kernel suits the call: give them no larger than need be (a
+ * step of few rows in a buffer for thousands gets the kernel for prompts, several times slower).  A captured call takes them as bounds and chooses by the lengths, in every replay.
  * Arithmetic: products of dtype inputs accumulated in fp32, softmax in fp32, out rounded to dtype. */
 fr_status fr_paged_attn(fr_ctx* ctx, const void* q, const int32_t* q_offsets, const int32_t* cached_len, int32_t n_requests,
                         int32_t n_tokens, int32_t max_new, const void* k_pages, const void* v_pages, int32_t n_pages,

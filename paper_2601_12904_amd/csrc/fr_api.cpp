@@ -943,6 +943,9 @@ fr_status fr_paged_attn(fr_ctx* ctx, const void* q, const int32_t* q_offsets, co
     a.max_new = max_new < n_tokens ? max_new : n_tokens;
     a.k_pages = k_pages; a.v_pages = v_pages; a.n_pages = n_pages; a.page_rows = page_rows;
     a.block_table = block_table; a.max_blocks = max_blocks; a.out = out; a.lse = lse_out; a.kernel = ctx->paged_kernel;
+    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+    if (hipStreamIsCapturing((hipStream_t)stream, &capture) != hipSuccess) (void)hipGetLastError();   // (the launch reports what is wrong with the stream)
+    a.captured = capture != hipStreamCaptureStatusNone;
     hipError_t e = launch_paged_attn(ctx->shape, a, ctx->ws.decode_partials, ctx->ws.n_cu, (hipStream_t)stream);
     if (e != hipSuccess) return hip_fail(ctx, "paged attention launch", e);
     return FR_OK;

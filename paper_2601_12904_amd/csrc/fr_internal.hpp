@@ -203,6 +203,7 @@ struct PagedAttnArgs {
     const int32_t* block_table; int max_blocks;
     void* out; float* lse;
     int kernel;   // FR_PAGED_KERNEL_*
+    bool captured;   // the stream is recording a graph: n_tokens and max_new bound the rows of its replays
 };
 size_t paged_attn_partials_bytes(const Shape& s, int n_cu);
 hipError_t launch_paged_attn(const Shape& s, const PagedAttnArgs& a, float* partials, int n_cu, hipStream_t st);

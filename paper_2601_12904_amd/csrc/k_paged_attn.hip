@@ -38,9 +38,13 @@ hipError_t launch_paged_attn(const Shape& s, const PagedAttnArgs& args, float* p
     a.cols_hi = INT32_MAX;
     if (args.kernel == FR_PAGED_KERNEL_TILED) return launch_paged_tile(s, a, n_cu, st);
     const int64_t rows = std::min<int64_t>(a.T, (int64_t)a.B * a.max_new);
-    // columns x keys of all KV heads (paged_route): no more than what the table has room for, no less than the chunks themselves (rows of no request are taken for some's)
-    const double most = (double)rows * s.Hq * a.cap, least = (double)rows * rows / a.B * s.Hq;
+    // columns x keys of all KV heads (paged_route).  No more than what the table has room for
+    const double most = (double)rows * s.Hq * a.cap;
     if ((int64_t)args.max_new * s.G <= a.few || most <= (double)PAGED_PAIRS_FAR) return launch_paged_stream(s, a, n_cu, st);
+    // and no less than the chunks themselves, the rows spread evenly (the sum of squares is least then) and those of requests with few columns taken off: if every row of the call is
+    // some request's.  A captured call has rows for the longest step it is replayed for, so there the lengths decide.
+    const double few_rows = (double)a.few / s.G;
+    const double least = args.captured || a.max_new > a.cap ? 0. : ((double)rows * rows / a.B - few_rows * few_rows * a.B) * s.Hq;
     a.together = (int64_t)(args.n_requests - 1) * s.Hkv <= n_cu / 4;
     a.route = least <= std::min((double)PAGED_PAIRS_NEAR, PAGED_PAIRS_SHORT + (double)PAGED_PAIRS_KEY * a.B * a.cap);
     if (a.route || !a.together) {
