@@ -360,8 +360,8 @@ fr_status fr_page_tables(fr_ctx* ctx, const int32_t* cached_len, const int32_t* 
 /* A step's rows into the pages: k_pages[slots[t]] = R(positions[t]) k_new[t], v_pages[slots[t]] = v_new[t], and
  * q_out[t] = R(positions[t]) q[t], with R the rotary embedding of the context's layer description.
  *   q            dev [n_tokens, Hq, d], not rotated, or NULL: keys and values only (q_out is NULL too)
- *   q_out        dev [n_tokens, Hq, d]; may equal q
- *   k_new, v_new dev [n_tokens, Hkv, d], not within the pages
+ *   q_out        dev [n_tokens, Hq, d]; may equal q, and otherwise overlaps nothing
+ *   k_new, v_new dev [n_tokens, Hkv, d]; like q and the index arrays not within the pages
  *   positions    dev [n_tokens] int32, or NULL: nothing is rotated, keys are stored bit for bit (rows of fr_qkv_rope)
  *   slots        dev [n_tokens] int32; a row whose slot lies outside the cache (such as -1) is stored nowhere, its q_out is written.
  *                No slot of the cache occurs twice

@@ -4,6 +4,7 @@
 #include <stdio.h>
 
 #include <algorithm>
+#include <initializer_list>
 #include <new>
 
 #include "fr_internal.hpp"
@@ -848,6 +849,20 @@ fr_status check_tokens(fr_ctx* ctx, int32_t n_tokens) {
     if (n_tokens > PAGED_MAX_POSITIONS) return fail(ctx, FR_ERR_UNSUPPORTED, "n_tokens = %d exceeds 2^30", n_tokens);
     return FR_OK;
 }
+// What a call writes lies beside what it reads and beside the rest of what it writes: its workgroups come in no order.
+struct Span { const char* name; const void* p; int64_t bytes; };
+fr_status check_apart(fr_ctx* ctx, std::initializer_list<Span> written, std::initializer_list<Span> read) {
+    auto meet = [](const Span& a, const Span& b) {
+        return a.p && b.p && a.bytes > 0 && b.bytes > 0 && (const char*)a.p < (const char*)b.p + b.bytes && (const char*)b.p < (const char*)a.p + a.bytes;
+    };
+    for (const Span* w = written.begin(); w != written.end(); ++w) {
+        for (const Span* o = w + 1; o != written.end(); ++o)
+            if (meet(*w, *o)) return fail(ctx, FR_ERR_INVALID_ARG, "%s and %s overlap, and both are written", w->name, o->name);
+        for (const Span& r : read)
+            if (meet(*w, r)) return fail(ctx, FR_ERR_INVALID_ARG, "%s is written and overlaps %s, which is read", w->name, r.name);
+    }
+    return FR_OK;
+}
 fr_status check_pages(fr_ctx* ctx, int32_t n_pages, int32_t page_rows) {
     if (n_pages < 0) return fail(ctx, FR_ERR_INVALID_ARG, "n_pages = %d is negative", n_pages);
     if (page_rows <= 0) return fail(ctx, FR_ERR_INVALID_ARG, "page_rows = %d is not positive", page_rows);
@@ -902,10 +917,16 @@ fr_status fr_paged_append(fr_ctx* ctx, const void* q, const void* k_new, const v
     if ((q == nullptr) != (q_out == nullptr)) return fail(ctx, FR_ERR_INVALID_ARG, "q and q_out must both be given or both be NULL");
     if (!aligned16(q) || !aligned16(q_out)) return fail(ctx, FR_ERR_INVALID_ARG, "q / q_out must be 16-byte aligned");
     if (q && !positions) return fail(ctx, FR_ERR_INVALID_ARG, "q is given but no positions to rotate it to");
-    const int64_t q_bytes = (int64_t)n_tokens * ctx->shape.Hq * ctx->shape.d * ctx->shape.esize;
+    const int64_t head_bytes = (int64_t)n_tokens * ctx->shape.d * ctx->shape.esize, q_bytes = head_bytes * ctx->shape.Hq, kv_bytes = head_bytes * ctx->shape.Hkv;
     if (q && q != q_out && (const char*)q < (const char*)q_out + q_bytes && (const char*)q_out < (const char*)q + q_bytes)
         return fail(ctx, FR_ERR_INVALID_ARG, "q and q_out overlap without being equal");
+    const int64_t cache_bytes = (int64_t)n_pages * page_rows * ctx->shape.Hkv * ctx->shape.d * ctx->shape.esize;
+    const Span keys{"k_pages", k_pages, cache_bytes}, values{"v_pages", v_pages, cache_bytes}, k_rows{"k_new", k_new, kv_bytes}, v_rows{"v_new", v_new, kv_bytes};
+    const Span at{"positions", positions, 4 * (int64_t)n_tokens}, to{"slots", slots, 4 * (int64_t)n_tokens};
+    if ((st = check_apart(ctx, {{"q_out", q_out, q_bytes}}, {keys, values, k_rows, v_rows, at, to})) != FR_OK) return st;
     if ((st = need_device(ctx)) != FR_OK) return st;
+    for (const Span& pages : {keys, values})   // (K and V pages may lie between one another, each page in one of the two)
+        if ((st = check_apart(ctx, {pages}, {{"q", q, q_bytes}, k_rows, v_rows, at, to})) != FR_OK) return st;
     PagedAppendArgs a;
     a.q = q; a.k = k_new; a.v = v_new; a.positions = positions; a.slots = slots; a.n_tokens = n_tokens;
     a.k_pages = k_pages; a.v_pages = v_pages; a.n_rows = (int64_t)n_pages * page_rows;
