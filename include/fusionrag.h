@@ -351,6 +351,7 @@ fr_status fr_mark_stale_rows(fr_ctx* ctx, uint32_t* stale_bits, int64_t n_words,
  *                max_blocks pages, and for those whose page the free list no longer had (its table entry is -1 then)
  *   pages_needed dev [1] int32: pages that the call takes, those that the list lacked included, or NULL.  The caller moves
  *                free_start on by it before the next step
+ * What the call writes overlaps neither what it reads (pages_needed is not free_start) nor the rest of what it writes.
  * Everything is a function of the inputs: a call that is repeated gives the same tables. */
 fr_status fr_page_tables(fr_ctx* ctx, const int32_t* cached_len, const int32_t* new_len, int32_t n_requests, int32_t page_rows,
                          const int32_t* free_pages, int32_t n_free, const int32_t* free_start, int32_t* block_table,

@@ -891,6 +891,11 @@ fr_status fr_page_tables(fr_ctx* ctx, const int32_t* cached_len, const int32_t* 
     if ((reinterpret_cast<uintptr_t>(free_start) & 3u) || (reinterpret_cast<uintptr_t>(pages_needed) & 3u))
         return fail(ctx, FR_ERR_INVALID_ARG, "free_start / pages_needed must be 4-byte aligned");
     if ((st = need_device(ctx)) != FR_OK) return st;
+    const int64_t tokens = 4 * (int64_t)n_tokens, requests = 4 * (int64_t)n_requests;
+    if ((st = check_apart(ctx, {{"block_table", block_table, requests * max_blocks}, {"q_offsets", q_offsets, requests + 4}, {"positions", positions, tokens},
+                                {"slots", slots, tokens}, {"pages_needed", pages_needed, 4}},
+                          {{"cached_len", cached_len, requests}, {"new_len", new_len, requests}, {"free_pages", free_pages, 4 * (int64_t)n_free}, {"free_start", free_start, 4}})) != FR_OK)
+        return st;
     PageTablesArgs a;
     a.cached_len = cached_len; a.new_len = new_len; a.n_requests = n_requests; a.page_rows = page_rows;
     a.free_pages = free_pages; a.n_free = n_free; a.free_start = free_start;

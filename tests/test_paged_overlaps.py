@@ -3,7 +3,7 @@ import pytest
 import torch
 
 from paper_2601_12904_amd import binding as B
-from tests.test_paged_host import APPEND, ARG, ctx, refused  # noqa: F401  (ctx is a fixture)
+from tests.test_paged_host import APPEND, ARG, TABLES, ctx, refused  # noqa: F401  (ctx is a fixture)
 
 M = 1 << 24
 FAR_APART = dict(APPEND, q=M, q_out=2 * M, k_new=3 * M, v_new=4 * M, positions=5 * M, slots=6 * M, k_pages=7 * M, v_pages=8 * M)
@@ -35,3 +35,14 @@ def test_append_of_arrays_side_by_side_is_not_refused(ctx):  # noqa: F811
 def test_append_from_within_the_pages(ctx, name, pages):  # noqa: F811
     """(Refused on the host: no kernel sees these addresses.)"""
     refused(ARG, ctx.fr_paged_append, FAR_APART, **{name: FAR_APART[pages] + 4096})
+
+
+TABLES_APART = dict(TABLES, **{name: (i + 1) * M for i, name in enumerate(("cached_len", "new_len", "free_pages", "free_start", "block_table", "q_offsets", "positions", "slots", "pages_needed"))})
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("written,other,at", [("pages_needed", "free_start", 0), ("pages_needed", "new_len", 8), ("q_offsets", "cached_len", -4), ("positions", "slots", 156),
+                                              ("slots", "new_len", -156), ("block_table", "free_pages", 16), ("q_offsets", "block_table", 92), ("pages_needed", "positions", 156)])
+def test_tables_on_top_of_one_another(ctx, written, other, at):  # noqa: F811
+    """(Refused on the host: no kernel sees these addresses.)"""
+    refused(ARG, ctx.fr_page_tables, TABLES_APART, **{written: TABLES_APART[other] + at})
