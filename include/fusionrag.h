@@ -376,7 +376,7 @@ fr_status fr_paged_append(fr_ctx* ctx, const void* q, const void* k_new, const v
  * prompts and whole prompts side by side.
  *   q            dev [n_tokens, Hq, d], rotated
  *   max_new      no request of the call has more rows than this (rows of a request beyond it are not computed)
- *   out          dev [n_tokens, Hq, d]; may equal q;  lse_out dev [n_tokens, Hq] fp32 natural-log normalisers, or NULL
+ *   out          dev [n_tokens, Hq, d]; may equal q;  lse_out dev [n_tokens, Hq] fp32 natural-log normalisers, or NULL.  Beyond that neither overlaps anything else
  * Rows of no request (q_offsets[n_requests] .. n_tokens - 1) are left as they were.  A position whose table entry is not a page
  * of the cache (0 .. n_pages - 1), or that lies beyond max_blocks pages, is invisible; a row that sees nothing at all (also: at a
  * negative position) has out = 0 and lse = -inf, as has one whose logits are all -inf.  Every finite logit counts.  What a row does not see has no

@@ -964,6 +964,13 @@ fr_status fr_paged_attn(fr_ctx* ctx, const void* q, const int32_t* q_offsets, co
     if (q != out && (const char*)q < (const char*)out + q_bytes && (const char*)out < (const char*)q + q_bytes)
         return fail(ctx, FR_ERR_INVALID_ARG, "q and out overlap without being equal");
     if ((st = need_device(ctx)) != FR_OK) return st;
+    const int64_t requests = 4 * (int64_t)n_requests, cache_bytes = (int64_t)n_pages * page_rows * ctx->shape.Hkv * ctx->shape.d * ctx->shape.esize;
+    const Span outputs{"out", out, q_bytes}, normalisers{"lse_out", lse_out, 4 * (int64_t)n_tokens * ctx->shape.Hq};
+    const Span keys{"k_pages", k_pages, cache_bytes}, values{"v_pages", v_pages, cache_bytes}, table{"block_table", block_table, requests * max_blocks};
+    const Span offsets{"q_offsets", q_offsets, requests + 4}, cached{"cached_len", cached_len, requests};
+    if ((st = check_apart(ctx, {outputs, normalisers}, {keys, values, table, offsets, cached})) != FR_OK ||
+        (st = check_apart(ctx, {normalisers}, {{"q", q, q_bytes}})) != FR_OK)
+        return st;
     PagedAttnArgs a{};
     a.q = q; a.q_offsets = q_offsets; a.cached_len = cached_len; a.n_requests = n_requests; a.n_tokens = n_tokens;
     a.max_new = max_new < n_tokens ? max_new : n_tokens;

@@ -3,7 +3,7 @@ import pytest
 import torch
 
 from paper_2601_12904_amd import binding as B
-from tests.test_paged_host import APPEND, ARG, TABLES, ctx, refused  # noqa: F401  (ctx is a fixture)
+from tests.test_paged_host import APPEND, ARG, ATTN, TABLES, ctx, refused  # noqa: F401  (ctx is a fixture)
 
 M = 1 << 24
 FAR_APART = dict(APPEND, q=M, q_out=2 * M, k_new=3 * M, v_new=4 * M, positions=5 * M, slots=6 * M, k_pages=7 * M, v_pages=8 * M)
@@ -46,3 +46,14 @@ TABLES_APART = dict(TABLES, **{name: (i + 1) * M for i, name in enumerate(("cach
 def test_tables_on_top_of_one_another(ctx, written, other, at):  # noqa: F811
     """(Refused on the host: no kernel sees these addresses.)"""
     refused(ARG, ctx.fr_page_tables, TABLES_APART, **{written: TABLES_APART[other] + at})
+
+
+ATTN_APART = dict(ATTN, **{name: (i + 1) * M for i, name in enumerate(("q", "q_offsets", "cached_len", "k_pages", "v_pages", "block_table", "out", "lse_out"))})
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("written,other,at", [("out", "k_pages", 1024), ("out", "v_pages", -64), ("out", "block_table", 32), ("out", "q_offsets", 0), ("lse_out", "out", 64), ("lse_out", "q", 4),
+                                              ("lse_out", "cached_len", 8), ("lse_out", "v_pages", 2048), ("lse_out", "q_offsets", 12)])
+def test_attention_on_top_of_what_it_reads(ctx, written, other, at):  # noqa: F811
+    """(Refused on the host: no kernel sees these addresses.)"""
+    refused(ARG, ctx.fr_paged_attn, ATTN_APART, **{written: ATTN_APART[other] + at})
