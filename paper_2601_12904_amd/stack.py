@@ -114,25 +114,32 @@ class PagedStack:
         self.Hq, self.Hkv, self.d = d.n_q_heads, d.n_kv_heads, d.head_dim
         # fr_qkv_rope rotates rows of this layout itself; others are projected part by part and rotated on the way into the pages
         self.fused_rope = d.head_dim == 128 and d.rope_layout == B.FR_ROPE_INTERLEAVED
-        self._buf, self._captured = {}, []
+        self._buf, self._captured = {}, {}
 
     def _scratch(self, T: int, n: int):
         capturing = torch.cuda.is_current_stream_capturing()
         if not capturing and self._buf.get("key") == (T, n):
             return self._buf
+        if capturing and (T, n) in self._captured:
+            return self._captured[T, n]
         mk = lambda *shape: torch.empty(shape, dtype=torch.bfloat16, device="cuda")
         i32 = lambda m: torch.empty(m, dtype=torch.int32, device="cuda")
         buf = dict(key=(T, n), x=mk(T, self.hidden), q=mk(T, self.Hq, self.d), k=mk(T, self.Hkv, self.d), v=mk(T, self.Hkv, self.d),
                    attn=torch.zeros((T, self.Hq, self.d), dtype=torch.bfloat16, device="cuda"), act=mk(T, self.ffn),
                    offsets=i32(n + 1), positions=i32(T), slots=i32(T))
         if capturing:
-            self._captured.append(buf)   # a graph's own, for as long as the stack lives: steps of other sizes do not free it
+            self._captured[T, n] = buf   # the graphs' of this size (the context's calls are in order, so they never run at once): steps of other sizes do not free it
         else:
             self._buf = buf
         return buf
 
+    def release(self):
+        """Gives back the buffers of all steps, captured ones too: for when no graph of this stack will be replayed again."""
+        self._buf, self._captured = {}, {}
+
     def forward(self, h: torch.Tensor, new_len: torch.Tensor, max_new: int, cache: PagedCache) -> torch.Tensor:
         """h [T, hidden] is updated in place and returned: the requests' rows one after the other, rows behind them hold nothing of use.
+        A captured step holds its buffers until release(); graphs of one size share them.
         new_len [n_requests] int32 on the device, none beyond max_new.  With head_dim 128 and interleaved pairs T is at most the
         context's max_tokens (fr_qkv_rope).  The cache's lengths and free list move on."""
         c, T, n = self.ctx, h.shape[0], cache.n_requests

@@ -57,3 +57,42 @@ def test_steps_against_the_oracles_layer(Hq, Hkv, d, half):
             H.assert_close(got[at: at + n], rows, "bf16", f"request {b}: rows")
             at += n
     ctx.close()
+
+
+def test_captures_of_one_size_share_their_buffers():
+    """A server that captures its step again and again holds one set of buffers for each size, and none after release()."""
+    Hq, Hkv, d, hidden, ffn, L, n = 8, 2, 128, 512, 256, 1, 2
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    layers = [S.random_layer(hidden, ffn, Hq, Hkv, d, gen, std=0.05) for _ in range(L)]
+    ctx = make_ctx((Hq, Hkv, d, "bf16"), tokens=4096)
+    stack = S.PagedStack(ctx, layers, hidden, ffn)
+    cache = S.PagedCache(L, n, 60, 8, 16, Hkv, d)
+    T, rows = 4096, torch.randn((3, hidden), generator=gen, device="cuda").bfloat16()
+    new = i32([0] * n)
+    h = torch.zeros((T, hidden), device="cuda").bfloat16()
+    stack.forward(h, new, 8, cache)          # (once outside)
+    torch.cuda.synchronize()
+    held, results = [], []
+    for _ in range(4):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            stack.forward(h, new, 8, cache)
+        for _ in range(2):
+            cache.cached_len.zero_(); cache.free_start.zero_()
+            new.copy_(i32([2, 1]))
+            h[:3] = rows
+            graph.replay()
+            torch.cuda.synchronize()
+            results.append(h[:3].clone())
+            new.zero_()
+            stack.forward(torch.zeros((5, hidden), device="cuda").bfloat16(), new, 5, cache)      # another size between the replays
+        held.append(torch.cuda.memory_allocated())
+        if len(held) < 4:
+            del graph
+    assert all(torch.equal(r, results[0]) for r in results) and bool(torch.isfinite(results[0].float()).all())
+    one = T * (hidden + Hq * d) * 2          # less than a set of buffers takes
+    assert held[-1] - held[0] < one, "captures of one size add up"
+    del graph
+    stack.release()
+    assert torch.cuda.memory_allocated() < held[0] - one
+    ctx.close()
