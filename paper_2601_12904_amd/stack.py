@@ -114,6 +114,8 @@ class PagedStack:
         self.Hq, self.Hkv, self.d = d.n_q_heads, d.n_kv_heads, d.head_dim
         # fr_qkv_rope rotates rows of this layout itself; others are projected part by part and rotated on the way into the pages
         self.fused_rope = d.head_dim == 128 and d.rope_layout == B.FR_ROPE_INTERLEAVED
+        if not self.fused_rope and (self.Hq * self.d % 128 or self.Hkv * self.d % 128):
+            raise ValueError(f"{self.Hq} / {self.Hkv} heads of {self.d}: queries, keys and values are projected by themselves, and fr_linear takes multiples of 128 features")
         self._buf, self._captured = {}, {}
 
     def _scratch(self, T: int, n: int):
