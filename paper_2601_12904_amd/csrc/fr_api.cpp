@@ -153,11 +153,14 @@ fr_status fr_create(const fr_layer_desc* desc, int64_t max_tokens, int32_t max_c
     const size_t o_img = take(w.kv_images_bytes);
     w.attn_partials_bytes = tiled ? attn_mfma_partials_bytes(s, max_tokens) : 0;
     const size_t o_part = take(w.attn_partials_bytes);
-    const size_t o_dpart = take(std::max(decode_partials_bytes(s), paged_attn_partials_bytes(s, w.n_cu)));
-    const size_t o_theta = take((size_t)(s.d / 2) * sizeof(double));
-    const size_t o_rr = take((size_t)max_tokens * (s.d / 2) * sizeof(float2));
+    const size_t o_dpart = take(decode_partials_bytes(s));
     w.gemm_partials_bytes = (s.dtype == FR_BF16) ? gemm_partials_bytes() : 0;
     const size_t o_gp = take(w.gemm_partials_bytes);
+    // partial results of fr_paged_attn: over those of decoding and of the projections, which no call uses beside them
+    const size_t paged_bytes = paged_attn_partials_bytes(s, w.n_cu);
+    if (off - o_dpart < paged_bytes) take(paged_bytes - (off - o_dpart));
+    const size_t o_theta = take((size_t)(s.d / 2) * sizeof(double));
+    const size_t o_rr = take((size_t)max_tokens * (s.d / 2) * sizeof(float2));
     // shapes whose kernels do not read a chunk store serve it through a gathered copy of the query's keys and values
     const size_t store_copy_bytes =
         attn_mfma_store_supported(s) ? 0 : (size_t)max_tokens * s.Hkv * s.d * s.esize;
@@ -190,6 +193,7 @@ fr_status fr_create(const fr_layer_desc* desc, int64_t max_tokens, int32_t max_c
     w.kv_images = (unsigned char*)(w.base + o_img);
     w.attn_partials = (float*)(w.base + o_part);
     w.decode_partials = (float*)(w.base + o_dpart);
+    w.paged_partials = (float*)(w.base + o_dpart);
     w.rope_theta = (double*)(w.base + o_theta);
     w.rope_rows = (float2*)(w.base + o_rr);
     w.gemm_partials = w.gemm_partials_bytes ? (float*)(w.base + o_gp) : nullptr;
@@ -979,7 +983,7 @@ fr_status fr_paged_attn(fr_ctx* ctx, const void* q, const int32_t* q_offsets, co
     hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
     if (hipStreamIsCapturing((hipStream_t)stream, &capture) != hipSuccess) (void)hipGetLastError();   // (the launch reports what is wrong with the stream)
     a.captured = capture != hipStreamCaptureStatusNone;
-    hipError_t e = launch_paged_attn(ctx->shape, a, ctx->ws.decode_partials, ctx->ws.n_cu, (hipStream_t)stream);
+    hipError_t e = launch_paged_attn(ctx->shape, a, ctx->ws.paged_partials, ctx->ws.n_cu, (hipStream_t)stream);
     if (e != hipSuccess) return hip_fail(ctx, "paged attention launch", e);
     return FR_OK;
 }

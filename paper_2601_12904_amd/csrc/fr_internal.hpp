@@ -54,7 +54,8 @@ struct Workspace {
     float* gemm_partials = nullptr; // partial sums of the GEMM tiles that are split along K
     size_t gemm_partials_bytes = 0;
     float2* rope_rows = nullptr;    // [max_tokens][d/2] (cos, sin) of the recomputed rows' positions
-    float* decode_partials = nullptr;    // partial softmax results: [DECODE_MAX_UNITS][Hq][d + 2] of fr_decode_attn's pieces, or those of fr_paged_attn
+    float* decode_partials = nullptr;    // [DECODE_MAX_UNITS][Hq][d + 2] partial softmax results of fr_decode_attn's pieces
+    float* paged_partials = nullptr;     // of fr_paged_attn's; over decode_partials and gemm_partials
     double* rope_theta = nullptr;        // [d/2] rotary frequencies base^(-2 (p + index_base) / d)
     float* attn_partials = nullptr;      // partial results of an attention launch whose items are computed in parts
     size_t attn_partials_bytes = 0;
