@@ -383,7 +383,8 @@ fr_status fr_paged_append(fr_ctx* ctx, const void* q, const void* k_new, const v
  * influence on it, whatever it holds.
  * Rows of no request cost next to nothing themselves, but n_tokens and max_new also tell the host which kernel suits the call: give them no larger than need be (a
  * step of few rows in a buffer for thousands gets the kernel for prompts, several times slower).  A captured call takes them as bounds and chooses by the lengths, in every replay.
- * Arithmetic: products of dtype inputs accumulated in fp32, softmax in fp32, out rounded to dtype. */
+ * Arithmetic: products of dtype inputs accumulated in fp32, softmax and its sums in fp32, out rounded to dtype; in bf16 each weight is rounded to bf16
+ * on its way into the product with the values (fr_decode_attn keeps 32 bits there), relative to the sum by half a step, 2^-8, of each at most. */
 fr_status fr_paged_attn(fr_ctx* ctx, const void* q, const int32_t* q_offsets, const int32_t* cached_len, int32_t n_requests,
                         int32_t n_tokens, int32_t max_new, const void* k_pages, const void* v_pages, int32_t n_pages,
                         int32_t page_rows, const int32_t* block_table, int32_t max_blocks, void* out, float* lse_out,

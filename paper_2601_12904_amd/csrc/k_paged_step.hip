@@ -2,7 +2,7 @@
 //
 // Tables.  off[b] = min(T, sum of new_len below b); request b takes its pages first_b = ceil(c_b / P) .. last_b - 1, last_b = ceil((c_b + n_b) / P),
 // n_b = off[b + 1] - off[b], from the free list behind those of the requests before it; row t of request b is position c_b + t - off[b].  A launch
-// of one kernel is all there is to it: every workgroup scans the lengths of all requests itself (16 KB at most, in the caches) rather than
+// of one kernel is all there is to it: every workgroup scans the lengths of all requests itself (32 KB at most, in the caches) rather than
 // wait for a pass that does, then every thread finds the request of its row, and of its page, by bisection in LDS.  The pages of a row are looked up
 // in the free list, not in the table that other threads are writing.  Latency: 4.4 us for 64 requests of a row each, 5.3 for 256 that bring 13 668; a launch of nothing is 4.
 //

@@ -7,7 +7,7 @@
 // prompt, which costs more: 512 rows from nothing, 32 / 8 heads, 31 us for 20, 1024 rows 77 for 41.)
 //
 // Measured, kernel alone: 64 rows behind 571 - 15757 positions (0.99 GB), 32 / 8 heads, 185 us = 5.4 TB/s; 32 times 2 - 8 rows behind 324 - 4902, 16 / 8 heads of 64 (0.14 GB), 31 us = 4.6 TB/s; one row behind
-// 4096 (17 MB) 9 us: the chain lengths -> table -> keys -> values -> merge; 254 rows in fp32, 4 heads of 64, 11 us.  The joining pass 3.9 - 7.9 us, of which a launch of nothing is 4.
+// 4096 (17 MB) 10 us: the chain lengths -> table -> keys -> values -> merge; 254 rows in fp32, 4 heads of 64, 11 us.  The joining pass 3.9 - 7.9 us, of which a launch of nothing is 4.
 //
 // S^T = K Q^T and O^T = V^T P^T with v_mfma_f32_16x16x32_bf16 (fp32: v_mfma_f32_16x16x4_f32), keys on the register dimension of S^T and columns on lanes: the accumulators of two 16-key
 // blocks are, after conversion, the B operand of the second product.  Row m of value product md is dim D / 16 m + md, so that a lane needs 16 (8)

@@ -8,8 +8,8 @@
 // Keys and values come straight from the pages, global -> LDS without registers: a wave brings eight consecutive rows of each tile, so in pages of a multiple of
 // eight rows their address is the same for the whole wave (scalar registers), and one table entry per wave and tile, itself copied to LDS two tiles
 // ahead, is all the look-up there is.  Rows lie in LDS as they do in memory, the 16-byte vectors of row r permuted by an exclusive or with r (the lanes ask for them
-// in that order), which keeps the fragment reads of both products free of bank conflicts: K by 16-byte reads, V^T by ds_read_b64_tr_b16, which
-// transposes 4 keys x 16 dims on the way.  So no pass packs or transposes anything in front: a chunk of 2048 rows behind 14336 would read, write and read
+// in that order), so that the rows of a fragment lie in different banks: K by 16-byte reads, V^T by ds_read_b64_tr_b16, which
+// transposes 4 keys x 16 dims on the way.  (Counted: a quarter of the LDS's active cycles are still conflicts, 260 of 1105 per tile; the loop over packed images has 6 of 665.)  So no pass packs or transposes anything in front: a chunk of 2048 rows behind 14336 would read, write and read
 // again 67 MB for it.
 //
 // A wave alternates between a matrix phase (O += its half of tile kt - 1, logits of its half of tile kt) and a softmax phase; the two waves of a SIMD do so in turn,
@@ -24,8 +24,9 @@
 // keys, found in a pass over them that forms nothing but logits.  Weights go into the second product as bf16 (half a step, 2^-8, of each; their sum is
 // taken in fp32 before), as the output does.
 //
-// Bound by the matrix instructions and the power they take: 3095 cycles per tile of 64 keys, 2048 of them matrix instructions of each SIMD, at 1.7 - 1.9 GHz under full load.  2048 rows
-// behind 14336 (32 / 8 heads, head_dim 128) 441 us = 1.17 PFLOP/s, 16896 from nothing 2004 us = 1.17 PFLOP/s; a library product of 8192^3 reaches 1.20.  An item takes
+// Bound by how well the loop feeds the matrix pipes: of 3450 cycles of a compute unit per tile of 64 keys (2048 rows behind 14336, everything counted; 3680 for 16896 from nothing) 2048 are matrix
+// instructions of each SIMD, 59 and 56 %.  2048 rows behind 14336 (32 / 8 heads, head_dim 128) 441 us = 1.17 PFLOP/s, 16896 from nothing 2020 us = 1.16; this library's prefill over a cache
+// of its own, which packs tile images first and then takes V by 16-byte reads and one of four query steps from LDS, does the same product in 1750 us with the packing, pipes busy 71 %.  An item takes
 // 17 us beside its tiles: plan, queries and page numbers 9, first copies and references 3, exchange and output 5.
 //
 // What a column does not see stays out of it by hand, as a weight of 0 does not take a NaN or an infinity out of a product: keys behind the tile's last row
@@ -43,7 +44,7 @@ constexpr int WAVES = 8, RG = 4, KT = 64, NC = 4;   // waves; row groups; keys o
 constexpr int C = 64 * RG;                          // columns of a tile
 constexpr int RW = KT / WAVES;                      // rows of a tile that a wave brings
 constexpr int TILE0 = 8;                            // ring slot of tile 0's page numbers; the others: tile % 8
-constexpr int ITEM_KEYS = 512;                      // what a piece costs beside its keys, in keys: 13 us of prologue, joining of the waves and output, a tile 1.5 us
+constexpr int ITEM_KEYS = 512;                      // what a piece costs beside its keys, in keys, a tile of 64 being 1.5 us: 12 of the 17 us above (the plan comes once for a workgroup)
 constexpr int MIN_SHARE = 1024;                     // a share smaller than this costs more to write and read as partial results than it saves
 
 typedef short __attribute__((ext_vector_type(4))) i16x4;
