@@ -120,13 +120,14 @@ class PagedStack:
 
     def _scratch(self, T: int, n: int):
         capturing = torch.cuda.is_current_stream_capturing()
-        if not capturing and self._buf.get("key") == (T, n):
+        key = T, n, torch.cuda.current_stream().cuda_stream   # (freed buffers go back to the stream that they were taken on: a step on another one takes its own)
+        if not capturing and self._buf.get("key") == key:
             return self._buf
         if capturing and (T, n) in self._captured:
             return self._captured[T, n]
         mk = lambda *shape: torch.empty(shape, dtype=torch.bfloat16, device="cuda")
         i32 = lambda m: torch.empty(m, dtype=torch.int32, device="cuda")
-        buf = dict(key=(T, n), x=mk(T, self.hidden), q=mk(T, self.Hq, self.d), k=mk(T, self.Hkv, self.d), v=mk(T, self.Hkv, self.d),
+        buf = dict(key=key, x=mk(T, self.hidden), q=mk(T, self.Hq, self.d), k=mk(T, self.Hkv, self.d), v=mk(T, self.Hkv, self.d),
                    attn=torch.zeros((T, self.Hq, self.d), dtype=torch.bfloat16, device="cuda"), act=mk(T, self.ffn),
                    offsets=i32(n + 1), positions=i32(T), slots=i32(T))
         if capturing:

@@ -96,3 +96,31 @@ def test_captures_of_one_size_share_their_buffers():
     stack.release()
     assert torch.cuda.memory_allocated() < held[0] - one
     ctx.close()
+
+
+def test_steps_on_two_streams_take_buffers_of_their_own():
+    """Steps on a second stream, behind one on the first: the first one's buffers, which go back to the first stream when they are dropped, are not among those that they use."""
+    Hq, Hkv, d, hidden, ffn, n = 8, 2, 128, 512, 256, 2
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    layers = [S.random_layer(hidden, ffn, Hq, Hkv, d, gen, std=0.05)]
+    ctx = make_ctx((Hq, Hkv, d, "bf16"), tokens=64)
+    stack = S.PagedStack(ctx, layers, hidden, ffn)
+    rows = torch.randn((3, hidden), generator=gen, device="cuda").bfloat16()
+    seen, append = {}, ctx.fr_paged_append
+
+    def spy(q, k_new, *rest):
+        seen.setdefault(torch.cuda.current_stream().cuda_stream, set()).add(k_new.data_ptr())
+        return append(q, k_new, *rest)
+    ctx.fr_paged_append = spy
+    got = []
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for i in (0, 1, 1, 0):
+        torch.cuda.synchronize()
+        with torch.cuda.stream(streams[i]):
+            cache = S.PagedCache(1, n, 20, 8, 8, Hkv, d)
+            got.append(stack.forward(rows.clone(), i32([2, 1]), 2, cache))
+    torch.cuda.synchronize()
+    assert all(torch.equal(g, got[0]) for g in got)
+    one, two = seen.values()
+    assert len(seen) == 2 and not one & two
+    ctx.close()
