@@ -51,6 +51,26 @@ def _int32(**arrays: Optional[torch.Tensor]):
             raise ValueError(f"{name} is of {t.dtype}: the library reads int32")
 
 
+def _sized(**arrays):
+    """(tensor or None, its length) each."""
+    for name, (t, n) in arrays.items():
+        if t is not None and t.shape != (n,):
+            raise ValueError(f"{name} has shape {tuple(t.shape)}, not ({n},)")
+
+
+def _rows(h: torch.Tensor, hidden: int, **beside: Optional[torch.Tensor]):
+    """h [T, hidden] as the library reads it, and what stands on the same device."""
+    if h.dim() != 2 or h.shape[1] != hidden:
+        raise ValueError(f"h has shape {tuple(h.shape)}, not (rows, {hidden})")
+    if h.dtype != torch.bfloat16:
+        raise ValueError(f"h is of {h.dtype}: the library reads bfloat16")
+    for name, t in beside.items():
+        if t is not None and t.device != h.device:
+            raise ValueError(f"{name}: on {t.device}, h on {h.device}")
+    if not h.is_cuda or h.device.index != torch.cuda.current_device():
+        raise ValueError(f"h: on {h.device}, not on the current GPU")
+
+
 def _normed(layers: List[LayerWeights]) -> bool:
     """Whether layers normalise queries and keys per head."""
     if any((w.q_norm is None) != (w.k_norm is None) for w in layers):
@@ -153,12 +173,21 @@ class Head:
             raise ValueError(f"{self.vocab} tokens, {self.hidden} features: fr_linear takes multiples of 128 and of 64")
         if rows_at_once < 1:
             raise ValueError(f"rows_at_once = {rows_at_once} is not positive")
+        _sized(g=(w.g, self.hidden))
+
+    def check(self, h: torch.Tensor, **beside: Optional[torch.Tensor]):
+        """Refuses rows that are not the head's, and arrays of another device (the library takes addresses)."""
+        if self.w.w.dtype != torch.bfloat16 or self.w.g.dtype != torch.bfloat16:
+            raise ValueError(f"the head's weights are of {self.w.w.dtype}, its norm of {self.w.g.dtype}: the library reads bfloat16")
+        _rows(h, self.hidden, weights=self.w.w, norm=self.w.g, **beside)
 
     def logprobs(self, h: torch.Tensor, tokens: Optional[torch.Tensor] = None, n_top: int = 1, scale: float = 1.0) -> dict:
         """Of the rows h [T, hidden] (fr_token_logprobs): "logprobs" [T] of the tokens, if any are given, "entropy" and "lse" [T], "top_ids" and "top_logprobs" [T, n_top];
         scale = 1 / temperature."""
         _int32(tokens=tokens)
         T = h.shape[0]
+        _sized(tokens=(tokens, T))
+        self.check(h, tokens=tokens)
         f32 = lambda *shape: torch.empty(shape, dtype=torch.float32, device=h.device)
         out = dict(logprobs=f32(T) if tokens is not None else None, entropy=f32(T), lse=f32(T),
                    top_ids=torch.empty((T, n_top), dtype=torch.int32, device=h.device), top_logprobs=f32(T, n_top))
