@@ -253,6 +253,9 @@ class PagedStack:
         new_len [n_requests] int32 on the device, none beyond max_new.  With head_dim 128 and interleaved pairs T is at most the
         context's max_tokens (fr_qkv_rope).  The cache's lengths and free list move on."""
         c, T, n = self.ctx, h.shape[0], cache.n_requests
+        _int32(new_len=new_len)
+        _sized(new_len=(new_len, n))
+        _rows(h, self.hidden, new_len=new_len)
         s = self._scratch(T, n)
         self._tables(new_len, T, cache, s)
 
@@ -275,9 +278,10 @@ class PagedStack:
         if max_new > B.FR_TREE_MAX_ROWS:
             raise ValueError(f"max_new = {max_new}: a tree has at most {B.FR_TREE_MAX_ROWS} rows")
         _int32(parents=parents, tokens=tokens, new_len=new_len, given=given)
-        for name, t, m in (("parents", parents, T), ("tokens", tokens, T), ("new_len", new_len, n), ("given", given, n)):
-            if t is not None and t.shape != (m,):
-                raise ValueError(f"{name} has shape {tuple(t.shape)}, not ({m},)")
+        _sized(parents=(parents, T), tokens=(tokens, T), new_len=(new_len, n), given=(given, n))
+        if head.hidden != self.hidden:
+            raise ValueError(f"a head of {head.hidden} features behind layers of {self.hidden}")
+        head.check(h, parents=parents, tokens=tokens, new_len=new_len, given=given)
         s = self._scratch(T, n)
         words = max(1, -(-max_new // 32))
         i32 = lambda *shape: torch.empty(shape, dtype=torch.int32, device=h.device)

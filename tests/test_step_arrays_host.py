@@ -55,3 +55,34 @@ def test_arrays_that_are_not_on_the_gpu_are_refused(ctx):
         S.Head(ctx, on(weights(), "meta")).logprobs(h.to("meta"), torch.zeros(6, dtype=I32))
     with pytest.raises(ValueError, match="weights: on cpu, h on meta"):
         S.Head(ctx, weights()).logprobs(h.to("meta"))
+
+
+def step(ctx, **change):
+    from types import SimpleNamespace
+    zeros = lambda n: torch.zeros(n, dtype=I32)
+    call = dict(h=torch.zeros((6, 64), dtype=BF), parents=zeros(6), tokens=zeros(6), new_len=zeros(2), max_new=3, cache=SimpleNamespace(n_requests=2), head=S.Head(ctx, weights()))
+    return dict(call, **change)
+
+
+@pytest.mark.parametrize("change,match", [
+    (dict(h=torch.zeros((6, 32), dtype=BF)), "h has shape"), (dict(h=torch.zeros((6, 64, 1), dtype=BF)), "h has shape"), (dict(h=torch.zeros(6, 64)), "h is of torch.float32"),
+    (dict(new_len=torch.zeros(2)), "int32"), (dict(new_len=torch.zeros(1, dtype=I32)), "new_len has shape"), (dict(new_len=torch.zeros(2, dtype=I32, device="meta")), "new_len: on meta"),
+    (dict(), "h: on cpu")])
+def test_steps_that_read_other_arrays_are_refused(ctx, change, match):
+    call = step(ctx, **change)
+    stack = S.PagedStack(ctx, [], 64, 64)
+    with pytest.raises(ValueError, match=match):
+        stack.verify(**call)
+    with pytest.raises(ValueError, match=match):
+        stack.forward(call["h"], call["new_len"], 3, call["cache"])
+
+
+@pytest.mark.parametrize("name", ["parents", "tokens", "given"])
+def test_drafts_of_another_device_are_refused(ctx, name):
+    with pytest.raises(ValueError, match=f"{name}: on meta"):
+        S.PagedStack(ctx, [], 64, 64).verify(**step(ctx, **{name: torch.zeros(2 if name == "given" else 6, dtype=I32, device="meta")}))
+
+
+def test_a_head_of_another_width_is_refused(ctx):
+    with pytest.raises(ValueError, match="128 features"):
+        S.PagedStack(ctx, [], 64, 64).verify(**step(ctx, head=S.Head(ctx, weights(hidden=128))))
