@@ -147,7 +147,7 @@ class SelectivePrefillStack:
 class PagedCache:
     """K/V of up to `n_requests` requests in pages of `page_rows` rows, for every layer; one free list and one block table serve all layers.
     Lengths and tables stay on the device (a captured step serves other lengths).  A step that asks for more pages than the list has
-    leaves the rows without one out of the cache: `free_start` is beyond `n_pages` then.  A request that ends is taken out by its
+    leaves the rows without one out of the cache: `free_start` is beyond `n_pages` then (verify() gives pages back and returns how far it was).  A request that ends is taken out by its
     length 0 and new entries of `free_pages`; the list may be rewritten between steps."""
 
     def __init__(self, n_layers: int, n_requests: int, n_pages: int, page_rows: int, max_blocks: int, Hkv: int, d: int,
@@ -272,8 +272,9 @@ class PagedStack:
         the first given[b] rows are not drafts but a chunk, each behind the one before.  h [T, hidden] as in forward; parents and tokens [T], new_len [n_requests] int32 on the device, none beyond
         max_new <= FR_TREE_MAX_ROWS.  The drafts stay that the model agrees with (its likeliest token after a row is a draft behind it), in every layer's pages at
         consecutive positions; the cache's lengths and free list move on by them alone.
-        Returns "kept" [n_requests] rows that stay, "path" [T] which ones they are, "next_token" [n_requests] the model's token behind them, and of every row "choice", its
-        likeliest token, "logprob" of it and "entropy"."""
+        Returns "kept" [n_requests] rows that stay, "path" [T] which ones they are, "next_token" [n_requests] the model's token behind them, "free_end" [1] the index in the
+        free list behind the pages that the step took (beyond cache.n_pages: the list was too short, and rows, kept ones perhaps among them, are not in the cache), and of every row
+        "choice", its likeliest token, "logprob" of it and "entropy"."""
         c, T, n = self.ctx, h.shape[0], cache.n_requests
         if max_new > B.FR_TREE_MAX_ROWS:
             raise ValueError(f"max_new = {max_new}: a tree has at most {B.FR_TREE_MAX_ROWS} rows")
@@ -295,11 +296,11 @@ class PagedStack:
         self._layers(h, positions, cache, s, attend)
         answer = head.logprobs(h)
         choice = answer["top_ids"].view(T)
-        cache.free_start += cache.pages_needed
+        free_end = cache.free_start + cache.pages_needed
         c.fr_tree_keep(parents, tokens, choice, s["offsets"], cache.cached_len, given, n, T, max_new, cache.k, cache.v, cache.n_pages, cache.page_rows, cache.block_table,
-                       cache.max_blocks, cache.free_pages, cache.n_pages, cache.free_start, cache.free_start, kept, path, next_token)
+                       cache.max_blocks, cache.free_pages, cache.n_pages, free_end, cache.free_start, kept, path, next_token)
         cache.cached_len += kept
-        return dict(kept=kept, path=path, next_token=next_token, choice=choice, logprob=answer["top_logprobs"].view(T), entropy=answer["entropy"])
+        return dict(kept=kept, path=path, next_token=next_token, free_end=free_end, choice=choice, logprob=answer["top_logprobs"].view(T), entropy=answer["entropy"])
 
     def _tables(self, new_len: torch.Tensor, T: int, cache: PagedCache, s: dict):
         self.ctx.fr_page_tables(cache.cached_len, new_len, cache.n_requests, cache.page_rows, cache.free_pages, cache.n_pages, cache.free_start, cache.block_table,
