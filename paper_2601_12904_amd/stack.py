@@ -280,6 +280,8 @@ class PagedStack:
             raise ValueError(f"max_new = {max_new}: a tree has at most {B.FR_TREE_MAX_ROWS} rows")
         _int32(parents=parents, tokens=tokens, new_len=new_len, given=given)
         _sized(parents=(parents, T), tokens=(tokens, T), new_len=(new_len, n), given=(given, n))
+        if len(cache.k) > B.FR_TREE_MAX_LAYERS:
+            raise ValueError(f"the cache has {len(cache.k)} layers: fr_tree_keep moves the rows of {B.FR_TREE_MAX_LAYERS} at most")
         if head.hidden != self.hidden:
             raise ValueError(f"a head of {head.hidden} features behind layers of {self.hidden}")
         head.check(h, parents=parents, tokens=tokens, new_len=new_len, given=given)

@@ -60,7 +60,7 @@ def test_arrays_that_are_not_on_the_gpu_are_refused(ctx):
 def step(ctx, **change):
     from types import SimpleNamespace
     zeros = lambda n: torch.zeros(n, dtype=I32)
-    call = dict(h=torch.zeros((6, 64), dtype=BF), parents=zeros(6), tokens=zeros(6), new_len=zeros(2), max_new=3, cache=SimpleNamespace(n_requests=2), head=S.Head(ctx, weights()))
+    call = dict(h=torch.zeros((6, 64), dtype=BF), parents=zeros(6), tokens=zeros(6), new_len=zeros(2), max_new=3, cache=SimpleNamespace(n_requests=2, k=[], v=[]), head=S.Head(ctx, weights()))
     return dict(call, **change)
 
 
@@ -86,3 +86,11 @@ def test_drafts_of_another_device_are_refused(ctx, name):
 def test_a_head_of_another_width_is_refused(ctx):
     with pytest.raises(ValueError, match="128 features"):
         S.PagedStack(ctx, [], 64, 64).verify(**step(ctx, head=S.Head(ctx, weights(hidden=128))))
+
+
+def test_more_layers_than_rows_can_be_kept_in_are_refused_before_the_step(ctx):
+    """(Behind the step, when fr_tree_keep refuses them, all of its work is lost.)"""
+    from types import SimpleNamespace
+    pages = [None] * (B.FR_TREE_MAX_LAYERS + 1)
+    with pytest.raises(ValueError, match="129 layers"):
+        S.PagedStack(ctx, [], 64, 64).verify(**step(ctx, cache=SimpleNamespace(n_requests=2, k=pages, v=pages)))
