@@ -163,7 +163,7 @@ def _open(arr, shared_query) -> ctypes.CDLL:
 
 def _ptr(t) -> Optional[int]:
     """Device address of a tensor (or a raw integer address, or None)."""
-    if t is None or type(t) is int:
+    if t is None or isinstance(t, int):
         return t
     if t.is_contiguous():
         return t.data_ptr()
@@ -172,7 +172,7 @@ def _ptr(t) -> Optional[int]:
 
 def _rows(t, rows: int, heads: int, d: int):
     """(address, elements from a row to the next) of rows whose heads are contiguous: a tensor [rows, heads, d] or a part of one, or an address of rows without gaps."""
-    if t is None or type(t) is int:
+    if t is None or isinstance(t, int):
         return t, heads * d
     between_rows, between_heads, between = t.stride()
     if between != 1 or (between_heads != d and heads > 1):
