@@ -429,6 +429,9 @@ fr_status fr_qk_norm_append(fr_ctx* ctx, const void* q, int64_t q_stride, const 
  * cached_len[b] + j, its row j, where bit j of its mask is set (j < the request's rows; bits beyond are ignored).  Any mask: fr_tree_tables makes those of
  * trees; an empty one leaves the cache, and a row that sees nothing at all has out = 0 and lse = -inf.
  *   mask, mask_words  mask_words >= ceil(max_new / 32)
+ * Which kernel a call takes follows from what the host knows: n_tokens, n_requests, max_new and the room of the table, max_blocks * page_rows; a captured call keeps it in every replay.  So short
+ * requests of more than 32 rows x heads of a group (64 with head_dim 64) behind a table with much room get the kernel for long ones, which takes 1 - 15 us longer there (16 requests of 24 rows behind 100 positions,
+ * 32 / 8 heads of 128, room for 131072: 24 us for 16): FR_OPT_PAGED_KERNEL chooses by hand.
  * Everything else as in fr_paged_attn. */
 fr_status fr_paged_tree_attn(fr_ctx* ctx, const void* q, const int32_t* q_offsets, const int32_t* cached_len, int32_t n_requests,
                              int32_t n_tokens, int32_t max_new, const uint32_t* mask, int32_t mask_words, const void* k_pages, const void* v_pages,

@@ -30,11 +30,15 @@ hipError_t launch_paged_attn(const Shape& s, const PagedAttnArgs& args, float* p
     a.scale_log2e = (1.0f / sqrtf((float)s.d)) * 1.4426950408889634f;
     a.mask = args.mask; a.words = args.mask_words;
     if (a.mask != nullptr) {
-        // A step with trees.  k_paged_tree.hip reads the keys once for 256 columns and takes 13 - 22 us for the shortest call, the streaming kernel once for 32 and 8 - 14 us.  us
-        // streaming : tree, requests x rows behind positions (columns of a request; columns x keys of all KV heads); 32 / 8 heads of 128: 1 x 16 behind 4000 (64; 2.1 M) 23 : 21,
-        // 1 x 64 behind 1000 (256; 2.2 M) 21 : 22, 16 x 24 behind 100 (96; 1.5 M) 16 : 26, 16 x 24 behind 1000 (12.6 M) 47 : 32, 16 x 40 behind 16000 (160; 328 M) 937 : 277, and with up to 32 columns
-        // 4 x 8 behind 4000 27 : 26, 16 x 8 behind 16000 210 : 206, 48 x 4 behind 1000 56 : 57; 16 / 8 heads of 64: 4 x 24 behind 16000 (48; 25 M) 43 : 46, 4 x 32 behind 1000 (64; 2.1 M) 21 : 23, 16 x 40 behind
-        // 1000 (80; 10.6 M) 25 : 25, 48 x 40 behind 4000 (80; 124 M) 242 : 117.
+        // A step with trees.  k_paged_tree.hip reads the keys once for 256 columns and takes 12 - 20 us for the shortest call, the streaming kernel once for 32 and 7 - 14 us.  us
+        // streaming : tree, requests x rows behind positions (columns of a request; columns x keys of all KV heads); 32 / 8 heads of 128: 1 x 16 behind 4000 (64; 2.1 M) 23 : 20,
+        // 1 x 64 behind 1000 (256; 2.2 M) 21 : 22, 16 x 24 behind 100 (96; 1.5 M) 16 : 24, 16 x 24 behind 1000 (12.6 M) 47 : 30, 16 x 40 behind 16000 (160; 328 M) 934 : 277, and with up to 32 columns
+        // 4 x 8 behind 4000 26 : 25, 16 x 8 behind 16000 207 : 204, 48 x 4 behind 1000 55 : 55; 16 / 8 heads of 64: 4 x 24 behind 16000 (48; 25 M) 43 : 42, 4 x 40 behind 1000 (80; 2.7 M) 19 : 21, 16 x 40 behind
+        // 1000 (80; 10.6 M) 25 : 24, 48 x 40 behind 4000 (80; 124 M) 242 : 111.
+        // Where the rule errs: of 375 calls (1 - 48 requests of one length, 2 - 128 rows behind 100 - 16000, those two and 28 / 4 heads of 128, tables as wide as the lengths) 14 take over 10 % longer than the other
+        // kernel would.  Many rows behind few keys or few columns behind many should stream: 4 x 128 behind 100 18 : 34, 16 x 64 behind 100 29 : 37, 1 x 128 behind 1000 23 : 29, 1 x 64 behind 4000 26 : 30, 28 / 4 heads 4 x 8
+        // behind 4000 22 : 28, 4 x 16 26 : 32, 1 x 16 behind 16000 27 : 33; long ones of head_dim 64 should not: 16 x 24 behind 16000 155 : 121, 48 x 24 behind 4000 116 : 102.  And it counts the room of
+        // the table, as the host does not know the lengths: with room for 131072 positions 69 of the 375 do, 59 of them behind 100 or 1000 (16 x 24 behind 100 16 : 24, 28 / 4 heads 16 : 31).
         a.cols_hi = INT32_MAX;
         const double pairs = (double)std::min<int64_t>(a.T, (int64_t)a.B * a.max_new) * s.Hq * a.cap;   // at most
         const bool many = (int64_t)a.max_new * s.G > (s.d == 128 ? 32 : 64) && pairs > (s.d == 128 ? 2.5e6 : 10e6);
