@@ -432,6 +432,8 @@ fr_status fr_qk_norm_append(fr_ctx* ctx, const void* q, int64_t q_stride, const 
  * Which kernel a call takes follows from what the host knows: n_tokens, n_requests, max_new and the room of the table, max_blocks * page_rows; a captured call keeps it in every replay.  So short
  * requests of more than 32 rows x heads of a group (64 with head_dim 64) behind a table with much room get the kernel for long ones, which takes 1 - 15 us longer there (16 requests of 24 rows behind 100 positions,
  * 32 / 8 heads of 128, room for 131072: 24 us for 16): FR_OPT_PAGED_KERNEL chooses by hand.
+ * Weights are up to 2^8 times that of a row's largest logit while they and the values are summed: out is what the formula says while the values that a row sees are at most 2^119 / (their
+ * number) in magnitude (2^95 for 2^24 of them); larger ones may give infinities.
  * Everything else as in fr_paged_attn. */
 fr_status fr_paged_tree_attn(fr_ctx* ctx, const void* q, const int32_t* q_offsets, const int32_t* cached_len, int32_t n_requests,
                              int32_t n_tokens, int32_t max_new, const uint32_t* mask, int32_t mask_words, const void* k_pages, const void* v_pages,
