@@ -464,6 +464,7 @@ fr_status fr_token_logprobs(fr_ctx* ctx, const void* logits, int32_t logits_dtyp
  *   n_given      dev [n_requests] int32, clamped to 1 .. the request's rows, or NULL: 1
  *   k_pages, v_pages  host [n_layers] of dev [n_pages][page_rows][Hkv][d]; n_layers <= FR_TREE_MAX_LAYERS, 0: nothing is moved
  *   block_table  dev [n_requests][max_blocks] int32, read only: the tables after fr_page_tables.  A row without a page is not moved, or not written
+ *                (where only the place that it would move to has one, that keeps what it held: another draft's row)
  *   free_pages   dev [n_free] int32, read and written: the pages that held positions of the step and hold none that stays (all of a request's behind
  *                ceil((cached_len[b] + kept_len_out[b]) / page_rows)) are put in front of index min(*free_end, n_free), by request and position.  They are in block_table still
  *   free_end     dev [1] int32: the index behind the pages that the step has taken (free_start + pages_needed), or NULL: no page is given back

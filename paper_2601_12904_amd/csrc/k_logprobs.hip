@@ -11,7 +11,7 @@
 // passes over the row.  The n best threads are found the same way: n / 4 rounds of a maximum in each of the four waves leave some 2 n of them to be counted (counting all 256 against one
 // another took 4 us, twice in a call of few rows).
 //
-// One alternative, as in greedy steps, needs no list: the largest of the threads' keys, whose holder looks at one vector again (8 rows 7.4 us for 10.7 by the list of one, 64 rows 11.3 for 14.7).
+// One alternative, as in greedy steps, needs no list: the largest of the threads' keys, whose holder looks at one vector again (8 rows 6.8 us, 64 rows 10.6; while both were there, the list of one took 3.3 us longer).
 //
 // Few rows: each row in parts, joined by a second launch in a fixed order.
 //

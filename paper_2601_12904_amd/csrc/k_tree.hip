@@ -7,7 +7,8 @@
 //
 // Keep.  The walk down a tree is a chain of one step per row that stays: one wave per request holds parents, tokens and choices in registers, a step
 // is a ballot over the rows.  A second launch moves the rows, a workgroup per request and layer, and puts pages back: both need walks that are over.  Calls of few requests are one launch: every
-// workgroup walks its own tree again, the one that sees to the pages walks all (16 requests, 2 layers: 12.6 us a call for 15.3, as a launch less is issued; captured, where issue does not count, 7.3 for 6.6).
+// workgroup walks its own tree again, the one that sees to the pages walks all (1 - 16 requests, 2 or 32 layers: 9.5 - 11.0 us a call for 13.6 - 14.7, as
+// a launch less is issued; captured, where issue does not count, 6.6 - 7.8 for 5.3 - 6.4.  With room for walks of 32 requests: 12.0 captured for 16 of them, 12.3 - 14.8 for 32).
 // Kept row i comes from row path[i] >= i, and path ascends, so no row is read behind a store to it (a thread moves its bytes of all rows, in their order).
 // Latency: 64 requests, 32 layers (31 MB read and written, at 5 TB/s 6 us) captured 9.9 us; the places of all rows are looked up beside the walk, or beside what it left.
 #include "fr_internal.hpp"

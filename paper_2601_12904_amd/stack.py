@@ -273,8 +273,8 @@ class PagedStack:
         max_new <= FR_TREE_MAX_ROWS.  The drafts stay that the model agrees with (its likeliest token after a row is a draft behind it), in every layer's pages at
         consecutive positions; the cache's lengths and free list move on by them alone.
         Returns "kept" [n_requests] rows that stay, "path" [T] which ones they are, "next_token" [n_requests] the model's token behind them, "free_end" [1] the index in the
-        free list behind the pages that the step took (beyond cache.n_pages: the list was too short, and rows, kept ones perhaps among them, are not in the cache), and of every row
-        "choice", its likeliest token, "logprob" of it and "entropy"."""
+        free list behind the pages that the step took (beyond cache.n_pages: the list was too short.  Rows without a page are not in the cache and do not see themselves, and where one of
+        them stays its position may hold another draft's row: such a request is best computed again), and of every row "choice", its likeliest token, "logprob" of it and "entropy"."""
         c, T, n = self.ctx, h.shape[0], cache.n_requests
         if max_new > B.FR_TREE_MAX_ROWS:
             raise ValueError(f"max_new = {max_new}: a tree has at most {B.FR_TREE_MAX_ROWS} rows")
